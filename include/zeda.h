@@ -257,6 +257,66 @@ int zeda_moe_block_forward(const zeda_layer_desc *desc, const void *xn, void *x_
                            const void *gamma_next, float eps, void *xn_next, int32_t *num_real_out, void *ws,
                            size_t ws_bytes, void *stream);
 
+/* ---------------------------------------------------------------------------------------------------------------------
+ * The layer with 8-bit experts: the expert weights of Section 2.1 in 8-bit floating point, for serving.  Values are e4m3 (the
+ * finite-only OCP format: largest magnitude 448, no infinities), and a block of 128 of them along the reduction dimension shares
+ * a scale, a power of two held as one byte s:  value = e4m3 * 2^(s - 127).  With Q(v) = rounding to the nearest such value
+ * (ties to even) under the least power of two that keeps the block's largest finite magnitude within 448 (at least 2^-126):
+ *        xq = Q(x) per token and 128 columns,   h = silu(G xq) .* (U xq),   E(x) = D Q(h),
+ * where G, U, D are stored under one scale per 128 x 128 block.  Products and sums are fp32 (the matrix instruction adds the 64
+ * products of one step with the bits that lie within about 13 binades of the largest of them: relative to the root mean square of
+ * a sum of 2048 that is 1.5e-5, far below the 2^-4 of the values themselves); h is rounded once, from fp32.  An infinity or
+ * no-number in x or h becomes a no-number and makes the token's expert outputs no-numbers; other tokens are not affected.
+ * Routing, dispatch, combine, x, the router and the result are those of the bf16 layer: desc->dtype must be ZEDA_BF16, and
+ * H and I at most 16384 (ZEDA_EUNSUPPORTED otherwise); desc->weight_layout is ignored.
+ * ------------------------------------------------------------------------------------------------------------------- */
+
+/* Rows to 8 bits: q[rows, cols] e4m3 and scales[rows, ceil(cols/128)] bytes from x[rows, cols] of `dtype` (zeda_dtype).  A last
+ * block may be shorter than 128.  cols % 8 == 0 (ZEDA_EUNSUPPORTED otherwise).  Infinities and no-numbers become no-numbers (0x7f,
+ * 0xff) and do not count for the scale.  rows = 0 is a no-op. */
+int zeda_quantize_rows_fp8(int32_t rows, int32_t cols, int32_t dtype, const void *x, void *q, uint8_t *scales, void *stream);
+
+/* Weights to 8 bits: `count` matrices w[count, rows, cols] of `dtype` to q[count, rows, cols] e4m3 under one scale per block of
+ * 128 x 128, scales[count, ceil(rows/128), ceil(cols/128)].  cols % 8 == 0.  Otherwise as zeda_quantize_rows_fp8. */
+int zeda_quantize_weights_fp8(int32_t count, int32_t rows, int32_t cols, int32_t dtype, const void *w, void *q, uint8_t *scales,
+                              void *stream);
+
+/* The experts' 8-bit weights in the layout that the kernels read (device pointers, 16-byte aligned; sizes in bytes from
+ * zeda_fp8_expert_bytes).  With Ip = I rounded up to 128, a 2 KiB unit holds 32 rows x 64 columns: the 16 bytes at row r, columns
+ * 32 p + 16 h of the unit stand at byte 1024 p + 16 (32 h + r).  w_gateup: N x (Ip/16) x (H/64) units, rows 0..15 of a unit gate rows, 16..31
+ * the up rows of the same index; w_down: N x (H/32) x (Ip/64) units.  s_gateup[N][Ip/128][gate, up][ceil4(H/128)],
+ * s_down[N][H/128][ceil4(Ip/128)]: scale bytes, rows filled up to multiples of four. */
+typedef struct {
+    void *w_gateup, *w_down, *s_gateup, *s_down;
+} zeda_fp8_experts;
+
+/* Sizes of the four buffers (host: size_t[4], in the struct's order).  desc->T is ignored. */
+int zeda_fp8_expert_bytes(const zeda_layer_desc *desc, size_t *bytes /* host */);
+
+/* One-time packing, from row-major e4m3 weights q_gate[N,I,H], q_up[N,I,H], q_down[N,H,I] with scales s_gate, s_up
+ * [N, ceil(I/128), H/128] and s_down[N, H/128, ceil(I/128)], as zeda_quantize_weights_fp8 writes them (or a checkpoint holds
+ * them).  Layout only: no value changes.  Scale bytes must be below 255.  in and out must not overlap.  desc->T is ignored. */
+int zeda_pack_expert_weights_fp8(const zeda_layer_desc *desc, const void *q_gate, const uint8_t *s_gate, const void *q_up,
+                                 const uint8_t *s_up, const void *q_down, const uint8_t *s_down, const zeda_fp8_experts *experts,
+                                 void *stream);
+
+/* zeda_expert_ffn, zeda_moe_forward and zeda_moe_block_forward with 8-bit experts: x (xn) is quantised inside; all other arguments,
+ * results and rules are those of the calls they stand beside.  Scratch: zeda_expert_ffn_workspace_bytes_fp8 and
+ * zeda_workspace_bytes_fp8; in the forward workspace topk_ids .. num_real lie at the offsets that zeda_workspace_layout_fp8 reports
+ * (`act` and `y_slot` hold the kernels' own forms: 8 bits, and fp16 under a power of two; only zeda_expert_ffn_fp8 gives bf16 rows). */
+size_t zeda_expert_ffn_workspace_bytes_fp8(const zeda_layer_desc *desc);
+size_t zeda_workspace_bytes_fp8(const zeda_layer_desc *desc);
+int zeda_workspace_layout_fp8(const zeda_layer_desc *desc, zeda_ws_layout *layout /* host */);
+int zeda_expert_ffn_fp8(const zeda_layer_desc *desc, const void *x, const zeda_fp8_experts *experts, const int32_t *expert_offsets,
+                        const int32_t *sorted_slot, const int32_t *num_real, void *y_slot /*[T*K,H]*/, void *ws, size_t ws_bytes,
+                        void *stream);
+int zeda_moe_forward_fp8(const zeda_layer_desc *desc, const void *x, const void *w_router, const float *router_bias,
+                         const zeda_fp8_experts *experts, void *out /*[T,H]*/, int32_t *num_real_out, void *ws, size_t ws_bytes,
+                         void *stream);
+int zeda_moe_block_forward_fp8(const zeda_layer_desc *desc, const void *xn, void *x_res, const void *w_router,
+                               const float *router_bias, const zeda_fp8_experts *experts, const void *gamma_next, float eps,
+                               void *xn_next, int32_t *num_real_out, void *ws, size_t ws_bytes, void *stream);
+
 /* Measurement aid, not part of the layer: reads `bytes` bytes of device memory at `buf` once, every workgroup a
  * contiguous 256 KiB run with 16-byte loads - the plainest streaming read there is.  Its rate on a buffer larger than
  * the caches is what HBM delivers to a kernel that does nothing else on this machine, the yardstick beside which

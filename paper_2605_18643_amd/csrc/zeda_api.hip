@@ -1,5 +1,6 @@
 // C ABI of libzeda: argument validation, workspace carving and the order of the launches.
 // The layer is Eq. 1 of Section 2.1; see include/zeda.h for the meaning of every argument.
+#include "zeda_fp8.h"
 #include "zeda_place.h"
 
 namespace zeda {
@@ -33,7 +34,8 @@ static size_t act_bytes(const zeda_layer_desc *d)
 static bool fused_counts(const zeda_layer_desc *d) { return route_counts_supported(d) && dispatch_counts_supported(d); }
 static size_t fused_counts_bytes(const zeda_layer_desc *d) { return fused_counts(d) ? route_counts_bytes(d) : 0; }
 
-static void layout_of(const zeda_layer_desc *d, zeda_ws_layout *L)
+// fp8: `act` is the scratch of the 8-bit experts
+static void layout_of(const zeda_layer_desc *d, zeda_ws_layout *L, bool fp8 = false)
 {
     const size_t S = (size_t)d->T * d->K;
     size_t o = 0;
@@ -46,10 +48,26 @@ static void layout_of(const zeda_layer_desc *d, zeda_ws_layout *L)
     L->num_real = take(4);
     // (the whole-layer call keeps the router's per-block counts here when it uses them instead of the counting pass)
     L->dispatch_ws = take(dispatch_ws_bytes(d) > fused_counts_bytes(d) ? dispatch_ws_bytes(d) : fused_counts_bytes(d));
-    L->act = take(act_bytes(d));
+    L->act = take(fp8 ? fp8_ffn_ws_bytes(d) : act_bytes(d));
     L->y_slot = take(S * d->H * elt_size(d));
     L->route_ws = take(route_ws_bytes(d));
     L->total = o;
+}
+
+// layers with 8-bit experts: what the kernels take besides what check_desc asks for
+static int check_desc_fp8(const zeda_layer_desc *d)
+{
+    if (!d) return ZEDA_EINVAL;
+    zeda_layer_desc r = *d;
+    r.weight_layout = ZEDA_WEIGHTS_ROW_MAJOR;
+    const int rc = check_desc(&r);
+    if (rc != ZEDA_OK) return rc;
+    return d->dtype == ZEDA_BF16 && d->H <= kFp8MaxWidth && d->I <= kFp8MaxWidth ? ZEDA_OK : ZEDA_EUNSUPPORTED;
+}
+static bool check_experts(const zeda_fp8_experts *e)
+{
+    return e && e->w_gateup && e->w_down && e->s_gateup && e->s_down && aligned16(e->w_gateup) && aligned16(e->w_down) &&
+           aligned16(e->s_gateup) && aligned16(e->s_down);
 }
 
 // one int32 written on the stream (a kernel rather than a memset node, so that captured graphs replay it reliably)
@@ -63,14 +81,15 @@ struct BlockTail {
     void *xn_next;
 };
 
-// out: the layer output, or NULL when tail is given
+// out: the layer output, or NULL when tail is given.  e8: 8-bit experts in place of w_gate, w_up, w_down (no events)
 static int forward_impl(const zeda_layer_desc *desc, const void *x, const void *w_router, const float *router_bias,
                         const void *w_gate, const void *w_up, const void *w_down, void *out, int32_t *num_real_out,
-                        void *ws, size_t ws_bytes, void *stream, void *const *events, const BlockTail *tail = nullptr)
+                        void *ws, size_t ws_bytes, void *stream, void *const *events, const BlockTail *tail = nullptr,
+                        const zeda_fp8_experts *e8 = nullptr)
 {
-    int rc = check_desc(desc);
+    int rc = e8 ? check_desc_fp8(desc) : check_desc(desc);
     if (rc != ZEDA_OK) return rc;
-    if (!x || !w_router || !w_gate || !w_up || !w_down || !ws) return ZEDA_EINVAL;
+    if (!x || !w_router || (!e8 && (!w_gate || !w_up || !w_down)) || !ws) return ZEDA_EINVAL;
     if (!aligned16(x) || !aligned16(w_router) || !aligned16(w_gate) || !aligned16(w_up) || !aligned16(w_down) ||
         !aligned16(ws) || (router_bias && !aligned16(router_bias)))
         return ZEDA_EINVAL;
@@ -83,7 +102,7 @@ static int forward_impl(const zeda_layer_desc *desc, const void *x, const void *
         return ZEDA_EINVAL;
     }
     zeda_ws_layout L;
-    layout_of(desc, &L);
+    layout_of(desc, &L, e8 != nullptr);
     if (ws_bytes < L.total) return ZEDA_EWORKSPACE;
     hipStream_t s = (hipStream_t)stream;
     char *w = (char *)ws;
@@ -112,7 +131,7 @@ static int forward_impl(const zeda_layer_desc *desc, const void *x, const void *
     const PlaceOut place = {offsets, sorted_slot, slot_to_row, num_real, num_real_out};
     // Few slots: the gate/up kernel places them, and selects for a handful of tokens (the tables it leaves are the same).
     TilePlace tp = {ids, place, gates, nullptr, router_bias, 0, 0, 0, desc->N + desc->Z, desc->gate_norm, false};
-    const bool places = gateup_places(desc);
+    const bool places = !e8 && gateup_places(desc);
     if (places) {
         if ((rc = launch_route(desc, x, w_router, router_bias, ids, gates, route_ws, nullptr, nullptr, gateup_selects(desc) ? &tp : nullptr, s)) != ZEDA_OK) return rc;
         mark(1 + ZEDA_STAGE_ROUTE);
@@ -130,13 +149,19 @@ static int forward_impl(const zeda_layer_desc *desc, const void *x, const void *
         if ((rc = launch_dispatch(desc, ids, offsets, sorted_slot, slot_to_row, num_real, num_real_out, w + L.dispatch_ws, s)) != ZEDA_OK) return rc;
     }
     mark(1 + ZEDA_STAGE_DISPATCH);
-    if ((rc = launch_gateup(desc, x, w_gate, w_up, offsets, sorted_slot, act, places ? &tp : nullptr, s)) != ZEDA_OK) return rc;
-    mark(1 + ZEDA_STAGE_GATEUP);
-    if ((rc = launch_down(desc, act, w_down, offsets, y_slot, s)) != ZEDA_OK) return rc;
+    const int16_t *y_exp = nullptr;
+    if (e8) {
+        if ((rc = launch_ffn_fp8(desc, x, e8, offsets, sorted_slot, y_slot, &y_exp, act, s)) != ZEDA_OK) return rc;
+    } else {
+        if ((rc = launch_gateup(desc, x, w_gate, w_up, offsets, sorted_slot, act, places ? &tp : nullptr, s)) != ZEDA_OK) return rc;
+        mark(1 + ZEDA_STAGE_GATEUP);
+        if ((rc = launch_down(desc, act, w_down, offsets, y_slot, s)) != ZEDA_OK) return rc;
+    }
     mark(1 + ZEDA_STAGE_DOWN);
-    rc = tail ? launch_combine_block(desc, y_slot, ids, gates, slot_to_row, x, tail->x_res, tail->gamma, tail->eps,
-                                     tail->xn_next, s)
-              : launch_combine(desc, y_slot, ids, gates, slot_to_row, x, out, s);
+    rc = tail    ? launch_combine_block(desc, y_slot, y_exp, ids, gates, slot_to_row, x, tail->x_res, tail->gamma, tail->eps,
+                                        tail->xn_next, s)
+         : y_exp ? launch_combine_scaled(desc, y_slot, y_exp, ids, gates, slot_to_row, x, out, s)
+                 : launch_combine(desc, y_slot, ids, gates, slot_to_row, x, out, s);
     if (rc != ZEDA_OK) return rc;
     mark(1 + ZEDA_STAGE_COMBINE);
     return rc;
@@ -508,6 +533,107 @@ int zeda_pack_expert_weights(const zeda_layer_desc *desc, const void *w_gate, co
         if (rc != ZEDA_OK) return rc;
     }
     return ZEDA_OK;
+}
+
+int zeda_quantize_rows_fp8(int32_t rows, int32_t cols, int32_t dtype, const void *x, void *q, uint8_t *scales, void *stream)
+{
+    if (rows < 0 || cols < 1 || (dtype != ZEDA_F32 && dtype != ZEDA_BF16) || !x || !q || !scales || !aligned16(x) || !aligned16(q)) return ZEDA_EINVAL;
+    if (cols % 8 != 0) return ZEDA_EUNSUPPORTED;
+    if (rows == 0) return ZEDA_OK;
+    return launch_quantize_rows(rows, cols, dtype, x, q, cols, scales, ceil_div(cols, kFp8Block), (hipStream_t)stream);
+}
+
+int zeda_quantize_weights_fp8(int32_t count, int32_t rows, int32_t cols, int32_t dtype, const void *w, void *q, uint8_t *scales, void *stream)
+{
+    if (count < 0 || rows < 1 || cols < 1 || (dtype != ZEDA_F32 && dtype != ZEDA_BF16) || !w || !q || !scales || !aligned16(w) || !aligned16(q))
+        return ZEDA_EINVAL;
+    if (cols % 8 != 0) return ZEDA_EUNSUPPORTED;
+    if (count == 0) return ZEDA_OK;
+    return launch_quantize_weights(count, rows, cols, dtype, w, q, scales, (hipStream_t)stream);
+}
+
+int zeda_fp8_expert_bytes(const zeda_layer_desc *desc, size_t *bytes)
+{
+    if (!desc || !bytes) return ZEDA_EINVAL;
+    zeda_layer_desc d = *desc;
+    d.T = 0;
+    const int rc = check_desc_fp8(&d);
+    if (rc != ZEDA_OK) return rc;
+    const size_t N = d.N, H = d.H, Ip = fp8_cols(d.I);
+    bytes[0] = N * 2 * Ip * H;
+    bytes[1] = N * H * Ip;
+    bytes[2] = N * (Ip / kFp8Block) * 2 * fp8_pitch(d.H);
+    bytes[3] = N * (H / kFp8Block) * fp8_pitch(d.I);
+    return ZEDA_OK;
+}
+
+int zeda_pack_expert_weights_fp8(const zeda_layer_desc *desc, const void *q_gate, const uint8_t *s_gate, const void *q_up,
+                                 const uint8_t *s_up, const void *q_down, const uint8_t *s_down, const zeda_fp8_experts *experts,
+                                 void *stream)
+{
+    size_t bytes[4];
+    const int rc = zeda_fp8_expert_bytes(desc, bytes);
+    if (rc != ZEDA_OK) return rc;
+    if (!q_gate || !s_gate || !q_up || !s_up || !q_down || !s_down || !check_experts(experts)) return ZEDA_EINVAL;
+    if (!aligned16(q_gate) || !aligned16(q_up) || !aligned16(q_down)) return ZEDA_EINVAL;
+    zeda_layer_desc d = *desc;
+    d.T = 0;
+    const size_t w = (size_t)d.N * d.I * d.H, sb = (size_t)d.N * ceil_div(d.I, kFp8Block) * (d.H / kFp8Block);
+    const struct { const void *p; size_t n; } in[6] = {{q_gate, w}, {q_up, w}, {q_down, w}, {s_gate, sb}, {s_up, sb}, {s_down, sb}},
+        out[4] = {{experts->w_gateup, bytes[0]}, {experts->w_down, bytes[1]}, {experts->s_gateup, bytes[2]}, {experts->s_down, bytes[3]}};
+    for (const auto &i : in)
+        for (const auto &o : out)
+            if ((const char *)i.p < (const char *)o.p + o.n && (const char *)o.p < (const char *)i.p + i.n) return ZEDA_EINVAL;  // overlap
+    return launch_pack_fp8(&d, (const uint8_t *)q_gate, s_gate, (const uint8_t *)q_up, s_up, (const uint8_t *)q_down, s_down, experts,
+                           (hipStream_t)stream);
+}
+
+size_t zeda_expert_ffn_workspace_bytes_fp8(const zeda_layer_desc *desc) { return check_desc_fp8(desc) == ZEDA_OK ? fp8_ffn_ws_bytes(desc) : 0; }
+
+int zeda_workspace_layout_fp8(const zeda_layer_desc *desc, zeda_ws_layout *layout)
+{
+    const int rc = check_desc_fp8(desc);
+    if (rc != ZEDA_OK) return rc;
+    if (!layout) return ZEDA_EINVAL;
+    layout_of(desc, layout, true);
+    return ZEDA_OK;
+}
+
+size_t zeda_workspace_bytes_fp8(const zeda_layer_desc *desc)
+{
+    zeda_ws_layout L;
+    return zeda_workspace_layout_fp8(desc, &L) == ZEDA_OK ? L.total : 0;
+}
+
+int zeda_expert_ffn_fp8(const zeda_layer_desc *desc, const void *x, const zeda_fp8_experts *experts, const int32_t *expert_offsets,
+                        const int32_t *sorted_slot, const int32_t *num_real, void *y_slot, void *ws, size_t ws_bytes, void *stream)
+{
+    const int rc = check_desc_fp8(desc);
+    if (rc != ZEDA_OK) return rc;
+    if (!x || !check_experts(experts) || !expert_offsets || !sorted_slot || !num_real || !y_slot || !ws) return ZEDA_EINVAL;
+    if (!aligned16(x) || !aligned16(expert_offsets) || !aligned16(sorted_slot) || !aligned16(y_slot) || !aligned16(ws)) return ZEDA_EINVAL;
+    if (ws_bytes < fp8_ffn_ws_bytes(desc)) return ZEDA_EWORKSPACE;
+    if (desc->T == 0) return ZEDA_OK;
+    // num_real equals expert_offsets[N], which the kernels read
+    return launch_ffn_fp8(desc, x, experts, expert_offsets, sorted_slot, y_slot, nullptr, ws, (hipStream_t)stream);
+}
+
+int zeda_moe_forward_fp8(const zeda_layer_desc *desc, const void *x, const void *w_router, const float *router_bias,
+                         const zeda_fp8_experts *experts, void *out, int32_t *num_real_out, void *ws, size_t ws_bytes, void *stream)
+{
+    if (!check_experts(experts)) return ZEDA_EINVAL;
+    return forward_impl(desc, x, w_router, router_bias, nullptr, nullptr, nullptr, out, num_real_out, ws, ws_bytes, stream, nullptr, nullptr,
+                        experts);
+}
+
+int zeda_moe_block_forward_fp8(const zeda_layer_desc *desc, const void *xn, void *x_res, const void *w_router, const float *router_bias,
+                               const zeda_fp8_experts *experts, const void *gamma_next, float eps, void *xn_next, int32_t *num_real_out,
+                               void *ws, size_t ws_bytes, void *stream)
+{
+    if (!check_experts(experts)) return ZEDA_EINVAL;
+    const BlockTail tail = {x_res, gamma_next, eps, xn_next};
+    return forward_impl(desc, xn, w_router, router_bias, nullptr, nullptr, nullptr, nullptr, num_real_out, ws, ws_bytes, stream, nullptr,
+                        &tail, experts);
 }
 
 int zeda_token_zero_slots(const zeda_layer_desc *desc, const int32_t *topk_ids, int32_t *zero_slots, int accumulate,

@@ -10,11 +10,14 @@
 // Block variant (FUSE): the workgroup holds the token's whole row, so in a pre-norm residual chain it also adds
 // the row to the residual stream in place and writes the RMSNorm of the new stream row, the next layer's
 // input: one pass over the row instead of three kernels.
+#include <type_traits>
+
 #include "zeda_internal.h"
 
 namespace zeda {
 
 constexpr int kCombineThreads = 256;
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 template <typename T> struct Vec;
 template <> struct Vec<bf16_t> {
@@ -31,8 +34,10 @@ constexpr int kFuseVecs = 4;
 
 // x_res, gamma, eps, xn_next: FUSE only.  x (the layer input, COPY only) and xn_next may be the same buffer:
 // a thread reads its pieces of a row before it writes them.
-template <typename T, bool COPY, bool FUSE>
-__global__ __launch_bounds__(kCombineThreads) void combine_kernel(const T *__restrict__ y_slot,
+// SCALED: y_slot holds fp16 under a power of two for every row and 128 columns, value = y * 2^y_exp[row][column / 128].
+template <typename T, bool COPY, bool FUSE, bool SCALED>
+__global__ __launch_bounds__(kCombineThreads) void combine_kernel(const std::conditional_t<SCALED, _Float16, T> *__restrict__ y_slot,
+                                                                  const int16_t *__restrict__ y_exp,
                                                                   const int32_t *__restrict__ ids,
                                                                   const float *__restrict__ gates,
                                                                   const int32_t *__restrict__ slot_to_row, const T *x,
@@ -90,15 +95,20 @@ __global__ __launch_bounds__(kCombineThreads) void combine_kernel(const T *__res
             // four rows at a time, so that their loads are in flight together; a padded entry is loaded (row 0, or
             // nothing but readable memory when there are no rows at all) and left out of the sum
             for (int j0 = 0; j0 < n; j0 += 4) {
-                vec_t y[4];
+                typedef std::conditional_t<SCALED, f16x8, vec_t> y_vec;
+                y_vec y[4];
+                int k[4];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) y[q] = *reinterpret_cast<const vec_t *>(y_slot + (size_t)s_row[j0 + q] * H + (size_t)v * VN);
+                for (int q = 0; q < 4; ++q) {
+                    y[q] = *reinterpret_cast<const y_vec *>(y_slot + (size_t)s_row[j0 + q] * H + (size_t)v * VN);
+                    if (SCALED) k[q] = y_exp[(size_t)s_row[j0 + q] * (H / 128) + v * VN / 128];
+                }
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
                     const bool use = j0 + q < n;
                     const float g = s_g[j0 + q];
 #pragma unroll
-                    for (int i = 0; i < VN; ++i) acc[i] = use ? fmaf(g, (float)y[q][i], acc[i]) : acc[i];
+                    for (int i = 0; i < VN; ++i) acc[i] = use ? fmaf(g, SCALED ? ldexpf((float)y[q][i], k[q]) : (float)y[q][i], acc[i]) : acc[i];
                 }
             }
             if (COPY) {
@@ -150,42 +160,35 @@ __global__ __launch_bounds__(kCombineThreads) void combine_kernel(const T *__res
     }
 }
 
-template <typename T>
-static void launch_combine_t(const zeda_layer_desc *d, const void *y_slot, const int32_t *ids, const float *gates,
-                             const int32_t *slot_to_row, const void *x, void *out, hipStream_t s)
+template <typename T, bool FUSE, bool SCALED>
+static void launch_combine_t(const zeda_layer_desc *d, const void *y_slot, const int16_t *y_exp, const int32_t *ids, const float *gates,
+                             const int32_t *slot_to_row, const void *x, void *out, void *x_res, const void *gamma, float eps, void *xn_next,
+                             hipStream_t s)
 {
+    typedef std::conditional_t<SCALED, _Float16, T> y_t;
     const int S = d->T * d->K, NE = d->N + d->Z;
     if (d->free_expert == ZEDA_EXPERT_COPY)
-        combine_kernel<T, true, false><<<d->T, kCombineThreads, 0, s>>>((const T *)y_slot, ids, gates, slot_to_row,
-                                                                       (const T *)x, (T *)out, d->H, d->N, NE, d->K, S,
-                                                                       nullptr, nullptr, 0.f, nullptr);
+        combine_kernel<T, true, FUSE, SCALED><<<d->T, kCombineThreads, 0, s>>>((const y_t *)y_slot, y_exp, ids, gates, slot_to_row, (const T *)x,
+                                                                              (T *)out, d->H, d->N, NE, d->K, S, (T *)x_res, (const T *)gamma,
+                                                                              eps, (T *)xn_next);
     else
-        combine_kernel<T, false, false><<<d->T, kCombineThreads, 0, s>>>((const T *)y_slot, ids, gates, slot_to_row,
-                                                                        nullptr, (T *)out, d->H, d->N, NE, d->K, S,
-                                                                        nullptr, nullptr, 0.f, nullptr);
-}
-
-template <typename T>
-static void launch_combine_block_t(const zeda_layer_desc *d, const void *y_slot, const int32_t *ids, const float *gates,
-                                   const int32_t *slot_to_row, const void *x, void *x_res, const void *gamma, float eps,
-                                   void *xn_next, hipStream_t s)
-{
-    const int S = d->T * d->K, NE = d->N + d->Z;
-    if (d->free_expert == ZEDA_EXPERT_COPY)
-        combine_kernel<T, true, true><<<d->T, kCombineThreads, 0, s>>>((const T *)y_slot, ids, gates, slot_to_row,
-                                                                      (const T *)x, nullptr, d->H, d->N, NE, d->K, S,
-                                                                      (T *)x_res, (const T *)gamma, eps, (T *)xn_next);
-    else
-        combine_kernel<T, false, true><<<d->T, kCombineThreads, 0, s>>>((const T *)y_slot, ids, gates, slot_to_row,
-                                                                       nullptr, nullptr, d->H, d->N, NE, d->K, S,
-                                                                       (T *)x_res, (const T *)gamma, eps, (T *)xn_next);
+        combine_kernel<T, false, FUSE, SCALED><<<d->T, kCombineThreads, 0, s>>>((const y_t *)y_slot, y_exp, ids, gates, slot_to_row, nullptr,
+                                                                               (T *)out, d->H, d->N, NE, d->K, S, (T *)x_res, (const T *)gamma,
+                                                                               eps, (T *)xn_next);
 }
 
 int launch_combine(const zeda_layer_desc *d, const void *y_slot, const int32_t *ids, const float *gates,
                    const int32_t *slot_to_row, const void *x, void *out, hipStream_t s)
 {
-    if (d->dtype == ZEDA_BF16) launch_combine_t<bf16_t>(d, y_slot, ids, gates, slot_to_row, x, out, s);
-    else launch_combine_t<float>(d, y_slot, ids, gates, slot_to_row, x, out, s);
+    if (d->dtype == ZEDA_BF16) launch_combine_t<bf16_t, false, false>(d, y_slot, nullptr, ids, gates, slot_to_row, x, out, nullptr, nullptr, 0.f, nullptr, s);
+    else launch_combine_t<float, false, false>(d, y_slot, nullptr, ids, gates, slot_to_row, x, out, nullptr, nullptr, 0.f, nullptr, s);
+    return last_launch_status();
+}
+
+int launch_combine_scaled(const zeda_layer_desc *d, const void *y_slot, const int16_t *y_exp, const int32_t *ids, const float *gates,
+                          const int32_t *slot_to_row, const void *x, void *out, hipStream_t s)
+{
+    launch_combine_t<bf16_t, false, true>(d, y_slot, y_exp, ids, gates, slot_to_row, x, out, nullptr, nullptr, 0.f, nullptr, s);
     return last_launch_status();
 }
 
@@ -195,13 +198,14 @@ bool combine_block_supported(const zeda_layer_desc *d)
     return d->H / vn <= kFuseVecs * kCombineThreads;
 }
 
-int launch_combine_block(const zeda_layer_desc *d, const void *y_slot, const int32_t *ids, const float *gates,
+int launch_combine_block(const zeda_layer_desc *d, const void *y_slot, const int16_t *y_exp, const int32_t *ids, const float *gates,
                          const int32_t *slot_to_row, const void *x, void *x_res, const void *gamma, float eps,
                          void *xn_next, hipStream_t s)
 {
     if (!combine_block_supported(d)) return ZEDA_EUNSUPPORTED;
-    if (d->dtype == ZEDA_BF16) launch_combine_block_t<bf16_t>(d, y_slot, ids, gates, slot_to_row, x, x_res, gamma, eps, xn_next, s);
-    else launch_combine_block_t<float>(d, y_slot, ids, gates, slot_to_row, x, x_res, gamma, eps, xn_next, s);
+    if (y_exp) launch_combine_t<bf16_t, true, true>(d, y_slot, y_exp, ids, gates, slot_to_row, x, nullptr, x_res, gamma, eps, xn_next, s);
+    else if (d->dtype == ZEDA_BF16) launch_combine_t<bf16_t, true, false>(d, y_slot, nullptr, ids, gates, slot_to_row, x, nullptr, x_res, gamma, eps, xn_next, s);
+    else launch_combine_t<float, true, false>(d, y_slot, nullptr, ids, gates, slot_to_row, x, nullptr, x_res, gamma, eps, xn_next, s);
     return last_launch_status();
 }
 

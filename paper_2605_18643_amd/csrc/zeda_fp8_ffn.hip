@@ -1,0 +1,356 @@
+// Grouped SwiGLU expert FFN over the real slots with 8-bit operands (Section 2.1; Appendix D, Eq. 10):
+//   xq = Q(x), h = silu(G xq) .* (U xq), y = D Q(h),
+// Q = rounding to e4m3 under a power-of-two scale for every 128 columns, G, U, D e4m3 under one for every 128 x 128 block.
+#include <type_traits>
+
+#include "zeda_fp8.h"
+#include "zeda_lds.h"
+#include "zeda_place.h"
+
+namespace zeda {
+
+constexpr int kF8Tok = 128;      // token rows of a tile
+constexpr int kF8Threads = 256;  // four waves, each two units (64 rows) of the weights against all token rows of the tile
+
+// One wave: {expert, first row, rows} of token tile `tile` of the expert-sorted rows, and the number of tiles of all experts.
+struct F8Tiles {
+    int off[5], nt[4], excl, total;
+    __device__ __forceinline__ void count(const int32_t *__restrict__ offsets, int N)
+    {
+        const int lane = threadIdx.x & 63;
+        int local = 0;
+#pragma unroll
+        for (int q = 0; q < 5; ++q) off[q] = offsets[min(4 * lane + q, N)];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            nt[q] = (off[q + 1] - off[q] + kF8Tok - 1) / kF8Tok;
+            local += nt[q];
+        }
+        const int incl = wave_scan(local);
+        excl = incl - local;
+        total = __builtin_amdgcn_readlane(incl, 63);
+    }
+    __device__ __forceinline__ int3 locate(int tile) const
+    {
+        int e = 0, row0 = 0, rows = 0, at = excl;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            if (tile >= at && tile < at + nt[q]) {
+                e = 4 * (threadIdx.x & 63) + q;
+                row0 = off[q] + (tile - at) * kF8Tok;
+                rows = min(kF8Tok, off[q + 1] - row0);
+            }
+            at += nt[q];
+        }
+        const int src = __ffsll((long long)__ballot(rows > 0)) - 1;
+        return make_int3(__builtin_amdgcn_readlane(e, src), __builtin_amdgcn_readlane(row0, src), __builtin_amdgcn_readlane(rows, src));
+    }
+};
+
+struct F8Args {
+    const uint8_t *src, *src_s;  // operand rows of ld bytes and their scales
+    const uint8_t *w, *ws;       // packed weights and scales
+    const int32_t *offsets, *sorted_slot;
+    uint8_t *act, *act_s;  // gate/up's result
+    void *y;               // down's
+    int16_t *y_exp;
+    int N, K, H, Ip, nft;  // nft: feature tiles
+    int log_terms;         // down: 2^log_terms >= Ip * 448 * 448
+};
+
+// What a launch leaves: activations, expert outputs in bf16, or (whole layer) expert outputs for the combine in the same 16 bits
+// but with 11 significant ones: fp16 under a power of two for every row and 128 columns that bounds the sum whatever its terms,
+// 2^k with k = the largest exponent of the blocks' scale products + log2(terms * 448^2) - 15.  bf16's 8 bits would cost the layer's
+// output a second rounding of the size of its own (2.6e-3 off in all, against 1.7e-3 for the rounding of the result alone).
+enum { kF8GateUp = 0, kF8Down = 1, kF8DownScaled = 2 };
+
+constexpr int kF8Slot = kF8Tok * kFp8Block, kF8Ring = 3 * kF8Slot;
+
+// Gate/up: 128 activations (256 weight rows, eight units) a workgroup; down: 256 output columns.
+template <int KIND>
+struct F8Kernel {
+    static constexpr bool GATEUP = KIND == kF8GateUp;
+    const F8Args &a;
+    uint8_t *ring, *tab;  // LDS: three chunks of token rows; the rows' scales and the weights'
+    int e, row0, rows, ft;
+
+    template <int NB>
+    __device__ __forceinline__ void run() const
+    {
+        const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l32 = lane & 31, half = lane >> 5;
+        const int ld = GATEUP ? a.H : a.Ip, nk = ld / kFp8Block, pitch = fp8_pitch(ld);
+        // the wave's two units: along the packed row blocks, clamped where the last feature tile is narrower
+        const int rbs = GATEUP ? a.Ip / 16 : a.H / 32, rb = ft * 8 + wave * 2;
+        const uint8_t *wp[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) wp[u] = a.w + ((size_t)e * rbs + min(rb + u, rbs - 1)) * (2 * nk) * kFp8Unit + lane * 16;
+        // This thread's piece of the token rows of every 32-row block: row tid / 8, and the ring's position tid % 8 of that row, where
+        // the row's 16-byte pieces stand permuted by the row: 16 lanes that read one piece of 16 rows touch all banks once.
+        const uint8_t *tp[NB];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+            const int r = row0 + min(32 * b + (tid >> 3), rows - 1);
+            tp[b] = a.src + (size_t)(GATEUP ? a.sorted_slot[r] / a.K : r) * ld + (((tid & 7) ^ ((tid >> 4) & 7)) << 4);
+        }
+        // scales: one LDS row per token row, then one (two: gate, up) for the weights
+        for (int i = tid; i < NB * 32 * (pitch / 4); i += kF8Threads) {
+            const int r = i / (pitch / 4), c = i - r * (pitch / 4), rr = row0 + min(r, rows - 1);
+            reinterpret_cast<uint32_t *>(tab)[i] =
+                reinterpret_cast<const uint32_t *>(a.src_s + (size_t)(GATEUP ? a.sorted_slot[rr] / a.K : rr) * pitch)[c];
+        }
+        uint8_t *wtab = tab + kF8Tok * pitch;
+        {
+            // (down: a workgroup's 256 rows are two blocks of 128)
+            const size_t r0 = GATEUP ? ((size_t)e * (a.Ip / kFp8Block) + ft) * 2 : (size_t)e * (a.H / kFp8Block) + ft * 2;
+            const int last = GATEUP ? 1 : min(1, a.H / kFp8Block - 1 - ft * 2);
+            for (int i = tid; i < 2 * (pitch / 4); i += kF8Threads) {
+                const int r = i / (pitch / 4), c = i - r * (pitch / 4);
+                reinterpret_cast<uint32_t *>(wtab)[i] = reinterpret_cast<const uint32_t *>(a.ws + (r0 + min(r, last)) * pitch)[c];
+            }
+        }
+        const uint32_t my_ws = lds_addr(wtab + (GATEUP ? l32 >> 4 : wave >> 1) * pitch), my_ts = lds_addr(tab + l32 * pitch);
+
+        f32x16 acc[2][NB];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) acc[u][b][i] = 0.f;
+
+        // Per chunk of 128 columns a wave fetches its weights into registers, one chunk ahead, and a quarter of the token rows
+        // into the ring, two chunks ahead.  Loads return in order, so a wave that has used chunk c's weights has the token rows
+        // of chunk c + 1 in the ring.
+        u32x4 wa[2][2][4];
+        auto load_w = [&](u32x4 (&d)[2][4], int c) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) d[u][q] = *reinterpret_cast<const u32x4 *>(wp[u] + (size_t)c * (2 * kFp8Unit) + q * 1024);
+        };
+        auto load_t = [&](int c, int slot) {
+#pragma unroll
+            for (int b = 0; b < NB; ++b)
+                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(tp[b] + (size_t)c * kFp8Block),
+                                                 (__attribute__((address_space(3))) void *)(ring + slot * kF8Slot + b * 4096 + wave * 1024), 16, 0, 0);
+        };
+        const uint32_t ring0 = lds_addr(ring), sw = (l32 >> 1) & 7;
+        uint32_t ts[NB], wsc = 0;  // four chunks' scales
+        auto multiply = [&](const u32x4 (&w)[2][4], int c, int slot) {
+            if ((c & 3) == 0) {
+                wsc = lds_read_b32(my_ws + c);
+#pragma unroll
+                for (int b = 0; b < NB; ++b) ts[b] = lds_read_b32(my_ts + 32 * b * pitch + c);
+                lds_wait(wsc);
+#pragma unroll
+                for (int b = 0; b < NB; ++b) lds_wait(ts[b]);
+            }
+            const int sa = (int)(wsc >> (8 * (c & 3)));
+            const uint32_t at = ring0 + slot * kF8Slot + l32 * kFp8Block;
+            u32x4 t[2][2];
+            auto fetch = [&](u32x4 (&d)[2], int s) {  // step s: half s % 2 of the chunk's columns of token block s / 2
+                d[0] = lds_read_b128(at + (s >> 1) * 4096 + (((4 * (s & 1) + half) ^ sw) << 4));
+                d[1] = lds_read_b128(at + (s >> 1) * 4096 + (((4 * (s & 1) + 2 + half) ^ sw) << 4));
+            };
+            fetch(t[0], 0);
+#pragma unroll
+            for (int s = 0; s < 2 * NB; ++s) {
+                if (s + 1 < 2 * NB) {
+                    fetch(t[(s + 1) & 1], s + 1);
+                    lds_wait_but<2>(t[s & 1][0], t[s & 1][1]);
+                } else {
+                    lds_wait(t[s & 1][0], t[s & 1][1]);
+                }
+                const int b = s >> 1, m = s & 1, sb = (int)(ts[b] >> (8 * (c & 3)));
+                const i32x8 tb = __builtin_bit_cast(i32x8, __builtin_shufflevector(t[s & 1][0], t[s & 1][1], 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const i32x8 wu = __builtin_bit_cast(i32x8, __builtin_shufflevector(w[u][2 * m], w[u][2 * m + 1], 0, 1, 2, 3, 4, 5, 6, 7));
+                    acc[u][b] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wu, tb, acc[u][b], 0, 0, 0, sa, 0, sb);
+                }
+            }
+        };
+        int slot = 0;
+        auto chunk = [&](const u32x4 (&w)[2][4], u32x4 (&next)[2][4], int c) {
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(NB + 8) : "memory");  // chunk c's token rows (behind them: chunk c + 1's, chunk c's weights)
+            asm volatile("s_barrier" ::: "memory");                        // everyone's; and everyone is done with chunk c - 1
+            load_t(min(c + 2, nk - 1), slot == 0 ? 2 : slot - 1);
+            load_w(next, min(c + 1, nk - 1));
+            multiply(w, c, slot);
+            slot = slot == 2 ? 0 : slot + 1;
+        };
+        load_t(0, 0);
+        load_t(min(1, nk - 1), 1);
+        load_w(wa[0], 0);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the scale tables are written (met by the first barrier)
+        for (int c = 0; c < nk; c += 2) {
+            chunk(wa[0], wa[1], c);
+            if (c + 1 < nk) chunk(wa[1], wa[0], c + 1);
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();  // everyone is done with the ring
+        // acc[u][b][i]: unit row 8 (i / 4) + 4 half + i % 4, token row 32 b + l32
+        if constexpr (GATEUP) {
+            float *s_max = reinterpret_cast<float *>(tab);  // [4][kF8Tok]
+            float h[2][NB][8], mx[NB];
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                mx[b] = 0.f;
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float g = acc[u][b][i];
+                        h[u][b][i] = g / (1.0f + __expf(-g)) * acc[u][b][i + 8];
+                        mx[b] = fmaxf(mx[b], finite_abs(h[u][b][i]));
+                    }
+                mx[b] = fmaxf(mx[b], __shfl_xor(mx[b], 32));
+                if (half == 0) s_max[wave * kF8Tok + 32 * b + l32] = mx[b];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                const int r = 32 * b + l32;
+                const int sb = scale_byte(fmaxf(fmaxf(s_max[r], s_max[kF8Tok + r]), fmaxf(s_max[2 * kF8Tok + r], s_max[3 * kF8Tok + r])));
+                const float inv = scale_inverse(sb);
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        const float *v = &h[u][b][4 * q];
+                        *reinterpret_cast<uint32_t *>(ring + r * kFp8Block + (((wave * 2 + u) ^ ((r >> 1) & 7)) << 4) + 8 * q + 4 * half) =
+                            to_e4m3(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+                    }
+                if (wave == 0 && half == 0 && r < rows) a.act_s[(size_t)(row0 + r) * fp8_pitch(a.Ip) + ft] = (uint8_t)sb;
+            }
+            __syncthreads();
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                const int r = 32 * b + (tid >> 3);
+                if (r < rows)
+                    *reinterpret_cast<u32x4_t *>(a.act + (size_t)(row0 + r) * a.Ip + ft * kFp8Block + (tid & 7) * 16) =
+                        *reinterpret_cast<const u32x4_t *>(ring + r * kFp8Block + (((tid & 7) ^ ((r >> 1) & 7)) << 4));
+            }
+        } else {
+            // a wave's 64 columns of 32 rows turn through 4 KiB of its own: whole cache lines leave
+            if (rb >= rbs) return;
+            uint8_t *buf = ring + wave * 4096;
+#pragma unroll
+            for (int b = 0; b < NB; ++b) {
+                int k = 0;
+                if constexpr (KIND == kF8DownScaled) {
+                    int most = 0;
+                    for (int c = 0; c < nk; ++c) most = max(most, (int)tab[(32 * b + l32) * pitch + c] + (int)wtab[(wave >> 1) * pitch + c]);
+                    k = most - 254 + a.log_terms - 15;
+                    if ((wave & 1) == 0 && half == 0 && 32 * b + l32 < rows)
+                        a.y_exp[(size_t)(row0 + 32 * b + l32) * (a.H / kFp8Block) + ft * 2 + (wave >> 1)] = (int16_t)k;
+                }
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        typedef std::conditional_t<KIND == kF8DownScaled, _Float16, bf16_t> out_t;
+                        typedef out_t out4 __attribute__((ext_vector_type(4)));
+                        out4 v;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) v[i] = (out_t)(KIND == kF8DownScaled ? ldexpf(acc[u][b][4 * q + i], -k) : acc[u][b][4 * q + i]);
+                        *reinterpret_cast<out4 *>(buf + l32 * 128 + (((4 * u + q) ^ ((l32 >> 1) & 7)) << 4) + 8 * half) = v;
+                    }
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int r = 8 * i + (lane >> 3);
+                    const u32x4_t v = *reinterpret_cast<const u32x4_t *>(buf + r * 128 + (((lane & 7) ^ ((r >> 1) & 7)) << 4));
+                    if (32 * b + r < rows) *reinterpret_cast<u32x4_t *>((uint16_t *)a.y + (size_t)(row0 + 32 * b + r) * a.H + rb * 32 + (lane & 7) * 8) = v;
+                }
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            }
+        }
+    }
+};
+
+template <int KIND>
+__global__ __launch_bounds__(kF8Threads, 2) void ffn_fp8_kernel(F8Args a)
+{
+    extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+    F8Tiles t;
+    t.count(a.offsets, a.N);
+    // the chip hands workgroups to its eight XCDs in turn: each takes a contiguous eighth of the items, so that the feature tiles of a
+    // token tile and the token tiles of an expert meet in one L2
+    const int items = t.total * a.nft, per = (items + 7) / 8, idx = blockIdx.x >> 3, item = (blockIdx.x & 7) * per + idx;
+    if (idx >= per || item >= items) return;
+    const int tile = item / a.nft, ft = item - tile * a.nft;
+    const int3 at = t.locate(tile);
+    const F8Kernel<KIND> k = {a, lds, lds + kF8Ring, at.x, at.y, at.z, ft};
+    const int nb = (at.z + 31) >> 5;
+    if (nb == 1) k.template run<1>();
+    else if (nb == 2) k.template run<2>();
+    else if (nb == 3) k.template run<3>();
+    else k.template run<4>();
+}
+
+// scratch: token rows and scales, activations and scales, exponents of the expert outputs
+struct F8Ws {
+    size_t x, xs, act, act_s, y_exp, total;
+};
+static F8Ws fp8_ws(const zeda_layer_desc *d)
+{
+    const size_t S = (size_t)d->T * d->K;
+    F8Ws w;
+    size_t o = 0;
+    auto take = [&](size_t bytes) { const size_t at = o; o += align_up(bytes ? bytes : 1, 256); return at; };
+    w.x = take((size_t)d->T * d->H);
+    w.xs = take((size_t)d->T * fp8_pitch(d->H));
+    w.act = take(S * fp8_cols(d->I));
+    w.act_s = take(S * fp8_pitch(d->I));
+    w.y_exp = take(S * (d->H / kFp8Block) * 2);
+    w.total = o;
+    return w;
+}
+size_t fp8_ffn_ws_bytes(const zeda_layer_desc *d) { return fp8_ws(d).total; }
+
+template <int KIND>
+static int launch_f8(const F8Args &a, int S, hipStream_t s)
+{
+    const int pitch = fp8_pitch(KIND == kF8GateUp ? a.H : a.Ip), tab = (kF8Tok + 2) * pitch, bytes = kF8Ring + (tab > 4 * kF8Tok * 4 ? tab : 4 * kF8Tok * 4);
+    static bool done[kMaxDevices] = {};  // per instantiation and device (idempotent)
+    const int dev = current_device();
+    if (dev < 0) return ZEDA_EHIP;
+    if (!done[dev]) {
+        constexpr int most = kF8Ring + (kF8Tok + 2) * (kFp8MaxWidth / kFp8Block);
+        if (hipFuncSetAttribute((const void *)ffn_fp8_kernel<KIND>, hipFuncAttributeMaxDynamicSharedMemorySize, most) != hipSuccess) return ZEDA_EHIP;
+        done[dev] = true;
+    }
+    const int64_t items = ((int64_t)S / kF8Tok + (a.N < S ? a.N : S)) * a.nft, grid = (items + 7) / 8 * 8;
+    if (grid > 0x7fffffff) return ZEDA_EUNSUPPORTED;
+    ffn_fp8_kernel<KIND><<<(unsigned)grid, kF8Threads, bytes, s>>>(a);
+    return last_launch_status();
+}
+
+int launch_ffn_fp8(const zeda_layer_desc *d, const void *x, const zeda_fp8_experts *e, const int32_t *offsets, const int32_t *sorted_slot,
+                   void *y_slot, const int16_t **y_exp, void *ws, hipStream_t s)
+{
+    const F8Ws L = fp8_ws(d);
+    uint8_t *w = (uint8_t *)ws;
+    const int S = d->T * d->K, Ip = fp8_cols(d->I);
+    int rc = launch_quantize_rows(d->T, d->H, d->dtype, x, w + L.x, d->H, w + L.xs, fp8_pitch(d->H), s);
+    if (rc != ZEDA_OK) return rc;
+    F8Args a = {};
+    a.offsets = offsets; a.sorted_slot = sorted_slot;
+    a.N = d->N; a.K = d->K; a.H = d->H; a.Ip = Ip;
+    a.src = w + L.x; a.src_s = w + L.xs;
+    a.w = (const uint8_t *)e->w_gateup; a.ws = (const uint8_t *)e->s_gateup;
+    a.act = w + L.act; a.act_s = w + L.act_s;
+    a.nft = Ip / kFp8Block;
+    if ((rc = launch_f8<kF8GateUp>(a, S, s)) != ZEDA_OK) return rc;
+    a.src = a.act; a.src_s = a.act_s;
+    a.w = (const uint8_t *)e->w_down; a.ws = (const uint8_t *)e->s_down;
+    a.y = y_slot;
+    a.nft = ceil_div(d->H, 256);
+    if (!y_exp) return launch_f8<kF8Down>(a, S, s);
+    *y_exp = a.y_exp = (int16_t *)(w + L.y_exp);
+    for (a.log_terms = 18; (1 << (a.log_terms - 18)) < Ip; ++a.log_terms) {}  // (448 * 448 < 2^18)
+    return launch_f8<kF8DownScaled>(a, S, s);
+}
+
+}  // namespace zeda

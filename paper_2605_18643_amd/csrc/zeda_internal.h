@@ -89,10 +89,14 @@ int launch_down_few(const zeda_layer_desc *d, const void *act, const void *wd, c
 int launch_pack_weights(const zeda_layer_desc *d, const void *w, void *out, bool down, hipStream_t s);
 int launch_combine(const zeda_layer_desc *d, const void *y_slot, const int32_t *ids, const float *gates,
                    const int32_t *slot_to_row, const void *x, void *out, hipStream_t s);
+// the same from fp16 rows under a power of two 2^y_exp[row][column / 128] for every 128 columns (bf16 layers)
+int launch_combine_scaled(const zeda_layer_desc *d, const void *y_slot, const int16_t *y_exp, const int32_t *ids, const float *gates,
+                          const int32_t *slot_to_row, const void *x, void *out, hipStream_t s);
 
+// (y_exp: NULL, or as in launch_combine_scaled)
 // combine fused with the pre-norm residual block: x_res += MoE output; xn_next (may be NULL) = RMSNorm(x_res) * gamma
 bool combine_block_supported(const zeda_layer_desc *d);
-int launch_combine_block(const zeda_layer_desc *d, const void *y_slot, const int32_t *ids, const float *gates,
+int launch_combine_block(const zeda_layer_desc *d, const void *y_slot, const int16_t *y_exp, const int32_t *ids, const float *gates,
                          const int32_t *slot_to_row, const void *x, void *x_res, const void *gamma, float eps,
                          void *xn_next, hipStream_t s);
 

@@ -27,7 +27,10 @@ EXPORTS = ("zeda_status_string", "zeda_workspace_bytes", "zeda_route_workspace_b
            "zeda_expert_ffn", "zeda_combine", "zeda_moe_forward", "zeda_moe_forward_events", "zeda_moe_block_forward",
            "zeda_rmsnorm",
            "zeda_residual_add", "zeda_pack_expert_weights", "zeda_routing_stats_workspace_bytes", "zeda_routing_stats",
-           "zeda_init_zero_expert_rows", "zeda_stream_read_probe", "zeda_mfma_probe", "zeda_token_zero_slots", "zeda_overlap_probe")
+           "zeda_init_zero_expert_rows", "zeda_stream_read_probe", "zeda_mfma_probe", "zeda_token_zero_slots", "zeda_overlap_probe",
+           "zeda_quantize_rows_fp8", "zeda_quantize_weights_fp8", "zeda_fp8_expert_bytes", "zeda_pack_expert_weights_fp8",
+           "zeda_expert_ffn_workspace_bytes_fp8", "zeda_workspace_bytes_fp8", "zeda_workspace_layout_fp8", "zeda_expert_ffn_fp8",
+           "zeda_moe_forward_fp8", "zeda_moe_block_forward_fp8")
 
 
 class LayerDesc(ctypes.Structure):
@@ -39,6 +42,16 @@ class WsLayout(ctypes.Structure):
     _fields_ = [(n, ctypes.c_size_t) for n in ("topk_ids", "topk_gates", "expert_offsets", "sorted_slot",
                                                "slot_to_row", "num_real", "dispatch_ws", "act", "y_slot", "route_ws",
                                                "total")]
+
+
+class Fp8Experts(ctypes.Structure):
+    """Packed 8-bit expert weights (zeda_fp8_experts): the C struct, and the device buffers that it points to in `buffers`."""
+
+    _fields_ = [(n, ctypes.c_void_p) for n in ("w_gateup", "w_down", "s_gateup", "s_down")]
+
+    def __init__(self, buffers):
+        super().__init__(*[b.data_ptr() for b in buffers])
+        self.buffers = tuple(buffers)
 
 
 class ZedaError(RuntimeError):
@@ -103,6 +116,26 @@ def lib() -> ctypes.CDLL:
         L.zeda_stream_read_probe.argtypes = [vp, sz, vp, vp]
         L.zeda_pack_expert_weights.restype = i32
         L.zeda_pack_expert_weights.argtypes = [dp, vp, vp, vp, vp, vp, vp, vp]
+        L.zeda_quantize_rows_fp8.restype = i32
+        L.zeda_quantize_rows_fp8.argtypes = [i32, i32, i32, vp, vp, vp, vp]
+        L.zeda_quantize_weights_fp8.restype = i32
+        L.zeda_quantize_weights_fp8.argtypes = [i32, i32, i32, i32, vp, vp, vp, vp]
+        ep = ctypes.POINTER(Fp8Experts)
+        L.zeda_fp8_expert_bytes.restype = i32
+        L.zeda_fp8_expert_bytes.argtypes = [dp, ctypes.POINTER(sz)]
+        L.zeda_pack_expert_weights_fp8.restype = i32
+        L.zeda_pack_expert_weights_fp8.argtypes = [dp, vp, vp, vp, vp, vp, vp, ep, vp]
+        for name in ("zeda_expert_ffn_workspace_bytes_fp8", "zeda_workspace_bytes_fp8"):
+            getattr(L, name).restype = sz
+            getattr(L, name).argtypes = [dp]
+        L.zeda_workspace_layout_fp8.restype = i32
+        L.zeda_workspace_layout_fp8.argtypes = [dp, ctypes.POINTER(WsLayout)]
+        L.zeda_expert_ffn_fp8.restype = i32
+        L.zeda_expert_ffn_fp8.argtypes = [dp, vp, ep, vp, vp, vp, vp, vp, sz, vp]
+        L.zeda_moe_forward_fp8.restype = i32
+        L.zeda_moe_forward_fp8.argtypes = [dp, vp, vp, vp, ep, vp, vp, vp, sz, vp]
+        L.zeda_moe_block_forward_fp8.restype = i32
+        L.zeda_moe_block_forward_fp8.argtypes = [dp, vp, vp, vp, vp, ep, vp, ctypes.c_float, vp, vp, vp, sz, vp]
         _lib = L
     return _lib
 
@@ -298,6 +331,85 @@ def zeda_pack_expert_weights(desc, w_gate, w_up, w_down, stream=None):
     _check(lib().zeda_pack_expert_weights(ctypes.byref(desc), _ptr(w_gate), _ptr(w_up), _ptr(w_down), _ptr(outs[0]),
                                           _ptr(outs[1]), _ptr(outs[2]), _stream(stream)), "zeda_pack_expert_weights")
     return tuple(outs)
+
+
+def _need(ok: bool, where: str) -> None:
+    """What the C side cannot see of a tensor (type, shape, strides)."""
+    if not ok:
+        raise ZedaError(ZEDA_EINVAL, where)
+
+
+def _is_float_buffer(t, dim: int) -> bool:
+    return t.dim() == dim and t.dtype in (torch.bfloat16, torch.float32) and t.is_contiguous()
+
+
+def zeda_quantize_rows_fp8(x, stream=None):
+    """x [rows, cols] (bf16 or fp32, contiguous) -> (q float8_e4m3fn [rows, cols], scales uint8 [rows, ceil(cols / 128)]):
+    x is nearly q * 2^(scale - 127)."""
+    _need(_is_float_buffer(x, 2), "zeda_quantize_rows_fp8")
+    rows, cols = x.shape
+    q = torch.empty((rows, cols), dtype=torch.float8_e4m3fn, device=x.device)
+    scales = torch.empty((rows, -(-cols // 128)), dtype=torch.uint8, device=x.device)
+    _check(lib().zeda_quantize_rows_fp8(rows, cols, _dtype_code(x), _ptr(x), _ptr(q), _ptr(scales), _stream(stream)), "zeda_quantize_rows_fp8")
+    return q, scales
+
+
+def zeda_quantize_weights_fp8(w, stream=None):
+    """w [count, rows, cols] (bf16 or fp32, contiguous) -> (q float8_e4m3fn like w, scales uint8 [count, ceil(rows / 128), ceil(cols / 128)])."""
+    _need(_is_float_buffer(w, 3), "zeda_quantize_weights_fp8")
+    count, rows, cols = w.shape
+    q = torch.empty((count, rows, cols), dtype=torch.float8_e4m3fn, device=w.device)
+    scales = torch.empty((count, -(-rows // 128), -(-cols // 128)), dtype=torch.uint8, device=w.device)
+    _check(lib().zeda_quantize_weights_fp8(count, rows, cols, _dtype_code(w), _ptr(w), _ptr(q), _ptr(scales), _stream(stream)),
+           "zeda_quantize_weights_fp8")
+    return q, scales
+
+
+def zeda_pack_expert_weights_fp8(desc, q_gate, s_gate, q_up, s_up, q_down, s_down, stream=None) -> Fp8Experts:
+    """The experts' 8-bit weights in the layout of the kernels (allocates the buffers); row-major inputs as
+    zeda_quantize_weights_fp8 gives them: q_gate, q_up [N, I, H], q_down [N, H, I]."""
+    N, H, I, Ib = desc.N, desc.H, desc.I, -(-desc.I // 128)
+    for t, shape in ((q_gate, (N, I, H)), (s_gate, (N, Ib, H // 128)), (q_up, (N, I, H)), (s_up, (N, Ib, H // 128)), (q_down, (N, H, I)),
+                     (s_down, (N, H // 128, Ib))):
+        _need(tuple(t.shape) == shape and t.element_size() == 1 and t.is_contiguous(), "zeda_pack_expert_weights_fp8")
+    sizes = (ctypes.c_size_t * 4)()
+    _check(lib().zeda_fp8_expert_bytes(ctypes.byref(desc), sizes), "zeda_fp8_expert_bytes")
+    e = Fp8Experts([torch.empty(n, dtype=torch.uint8, device=q_gate.device) for n in sizes])
+    _check(lib().zeda_pack_expert_weights_fp8(ctypes.byref(desc), _ptr(q_gate), _ptr(s_gate), _ptr(q_up), _ptr(s_up), _ptr(q_down), _ptr(s_down),
+                                              ctypes.byref(e), _stream(stream)), "zeda_pack_expert_weights_fp8")
+    return e
+
+
+def workspace_bytes_fp8(desc: LayerDesc) -> int:
+    return int(lib().zeda_workspace_bytes_fp8(ctypes.byref(desc)))
+
+
+def expert_ffn_workspace_bytes_fp8(desc: LayerDesc) -> int:
+    return int(lib().zeda_expert_ffn_workspace_bytes_fp8(ctypes.byref(desc)))
+
+
+def workspace_layout_fp8(desc: LayerDesc) -> WsLayout:
+    out = WsLayout()
+    _check(lib().zeda_workspace_layout_fp8(ctypes.byref(desc), ctypes.byref(out)), "zeda_workspace_layout_fp8")
+    return out
+
+
+def zeda_expert_ffn_fp8(desc, x, experts: Fp8Experts, expert_offsets, sorted_slot, num_real, y_slot, ws, stream=None) -> None:
+    _check(lib().zeda_expert_ffn_fp8(ctypes.byref(desc), _ptr(x), ctypes.byref(experts), _ptr(expert_offsets), _ptr(sorted_slot), _ptr(num_real),
+                                     _ptr(y_slot), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)), "zeda_expert_ffn_fp8")
+
+
+def zeda_moe_forward_fp8(desc, x, w_router, router_bias, experts: Fp8Experts, out, num_real_out, ws, stream=None) -> None:
+    _check(lib().zeda_moe_forward_fp8(ctypes.byref(desc), _ptr(x), _ptr(w_router), _ptr(router_bias), ctypes.byref(experts), _ptr(out),
+                                      _ptr(num_real_out), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)), "zeda_moe_forward_fp8")
+
+
+def zeda_moe_block_forward_fp8(desc, xn, x_res, w_router, router_bias, experts: Fp8Experts, gamma_next, eps: float, xn_next, num_real_out, ws,
+                               stream=None) -> None:
+    """zeda_moe_block_forward with 8-bit experts."""
+    _check(lib().zeda_moe_block_forward_fp8(ctypes.byref(desc), _ptr(xn), _ptr(x_res), _ptr(w_router), _ptr(router_bias), ctypes.byref(experts),
+                                            _ptr(gamma_next), float(eps), _ptr(xn_next), _ptr(num_real_out), _ptr(ws),
+                                            ws.numel() * ws.element_size(), _stream(stream)), "zeda_moe_block_forward_fp8")
 
 
 def ws_views(desc: LayerDesc, ws: torch.Tensor):
