@@ -317,6 +317,51 @@ int zeda_moe_block_forward_fp8(const zeda_layer_desc *desc, const void *xn, void
                                const float *router_bias, const zeda_fp8_experts *experts, const void *gamma_next, float eps,
                                void *xn_next, int32_t *num_real_out, void *ws, size_t ws_bytes, void *stream);
 
+/* ---------------------------------------------------------------------------------------------------------------------
+ * Training the router (Section 2.2): the balance losses with their gradient, and the gradient of the routing weights of Eq. 1.
+ * One training step: zeda_route_train, zeda_dispatch, zeda_expert_ffn (or zeda_expert_ffn_fp8: experts frozen in 8 bits),
+ * zeda_combine; then zeda_combine_backward and zeda_route_backward.
+ * ------------------------------------------------------------------------------------------------------------------- */
+
+/* zeda_route for a training step: topk_ids and topk_gates as there (the sums are those of zeda_route with scratch), and
+ *   probs[t,i] = softmax over all N+Z logits;
+ *   counts[i] = tokens with token_mask[t] != 0 whose top-K set holds expert i, n = their number, f[i] = counts[i] / n,
+ *   P[i] = mean of probs[t,i] over those tokens;  summary[0..6] as in zeda_routing_stats, with these f and P: f_E, P_E, f_Z, P_Z, r_ZE,
+ *   L_A (Eq. 4), L_GA (Eq. 5-6).
+ * token_mask[T] (bytes) may be NULL (every token counts); padding that does not count is routed all the same.  If nothing counts
+ * (T = 0 too, where the [T,..] arrays may be NULL), counts, P and summary are zero.  w > 0.  probs[T, N+Z], P, summary fp32, counts int32; topk_ids, topk_gates, probs
+ * 16-byte aligned.  ws: scratch of zeda_route_train_workspace_bytes(desc). */
+size_t zeda_route_train_workspace_bytes(const zeda_layer_desc *desc);
+int zeda_route_train(const zeda_layer_desc *desc, const void *x, const void *w_router, const float *router_bias,
+                     const uint8_t *token_mask /*[T]*/, float alpha, float w, int32_t *topk_ids /*[T,K]*/, float *topk_gates /*[T,K]*/,
+                     float *probs /*[T,N+Z]*/, int32_t *counts /*[N+Z]*/, float *P /*[N+Z]*/, float *summary /*[7]*/, void *ws,
+                     size_t ws_bytes, void *stream);
+
+/* Gradient of  d_loss[0] L_A + d_loss[1] L_GA + sum over t, j of d_gates[t,j] topk_gates[t,j]  with respect to the logits, carried on to
+ *   dx[T,H] (type of x), dw_router[N+Z,H] and dbias[N+Z] (fp32); any of the three may be NULL, not all.
+ * The top-K sets and f are constants, as in the losses' definition; desc->gate_norm says how the gates depend on the logits.
+ * probs, topk_ids, topk_gates, counts, token_mask, alpha, w: as zeda_route_train left and was given them.  d_loss[2] (device, fp32) and
+ * d_gates[T,K] (fp32): NULL for zero, not both.  A token with token_mask[t] == 0 takes no part whatever its entries hold (not-a-number
+ * included): its row of dx is zero and x[t] does not enter dw_router.  dx is overwritten (not added to) and must not overlap x or w_router.
+ * T = 0: dw_router and dbias are zero, the [T,..] arrays may be NULL.
+ * Sums run in a fixed order; fp32, of three bf16 parts of the logits' gradient for dw_router (nothing is lost) and of two for a bf16 dx.
+ * ws: scratch of zeda_route_backward_workspace_bytes(desc). */
+size_t zeda_route_backward_workspace_bytes(const zeda_layer_desc *desc);
+int zeda_route_backward(const zeda_layer_desc *desc, const void *x, const void *w_router, const float *probs, const int32_t *topk_ids,
+                        const float *topk_gates, const uint8_t *token_mask, const int32_t *counts, float alpha, float w,
+                        const float *d_loss /*[2]*/, const float *d_gates /*[T,K]*/, void *dx /*[T,H]*/, float *dw_router /*[N+Z,H]*/,
+                        float *dbias /*[N+Z]*/, void *ws, size_t ws_bytes, void *stream);
+
+/* Backward of zeda_combine: from d_out[T,H],
+ *   d_gates[t,j] = <d_out[t,:], y_slot[row,:]> for a slot on a normal expert (row = slot_to_row[t*K+j]), 0 for a zero expert;
+ *   d_y_slot[row,:] = topk_gates[t,j] d_out[t,:]  (may be NULL; rows past R are left as they are).
+ * ZEDA_EXPERT_COPY: d_gates of a slot on a free expert is <d_out[t,:], x[t,:]>, and dx[t,:] (may be NULL) = (sum of the token's gates on
+ * free experts) d_out[t,:], the copy term's own share of the gradient of x; otherwise x is not read and dx must be NULL.
+ * d_gates fp32 [T,K], the others of desc->dtype; outputs must not overlap inputs or each other.  T = 0 is a no-op. */
+int zeda_combine_backward(const zeda_layer_desc *desc, const void *d_out, const void *y_slot, const int32_t *topk_ids,
+                          const float *topk_gates, const int32_t *slot_to_row, const void *x, float *d_gates /*[T,K]*/,
+                          void *d_y_slot /*[T*K,H]*/, void *dx /*[T,H]*/, void *stream);
+
 /* Measurement aid, not part of the layer: reads `bytes` bytes of device memory at `buf` once, every workgroup a
  * contiguous 256 KiB run with 16-byte loads - the plainest streaming read there is.  Its rate on a buffer larger than
  * the caches is what HBM delivers to a kernel that does nothing else on this machine, the yardstick beside which

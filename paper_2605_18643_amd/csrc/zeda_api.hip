@@ -636,6 +636,71 @@ int zeda_moe_block_forward_fp8(const zeda_layer_desc *desc, const void *xn, void
                         &tail, experts);
 }
 
+static bool overlap(const void *a, size_t na, const void *b, size_t nb)
+{
+    return a && b && (const char *)a < (const char *)b + nb && (const char *)b < (const char *)a + na;
+}
+static bool aligned4(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+
+size_t zeda_route_train_workspace_bytes(const zeda_layer_desc *desc) { return check_desc(desc) == ZEDA_OK ? route_train_ws_bytes(desc) : 0; }
+
+int zeda_route_train(const zeda_layer_desc *desc, const void *x, const void *w_router, const float *router_bias, const uint8_t *token_mask,
+                     float alpha, float w, int32_t *topk_ids, float *topk_gates, float *probs, int32_t *counts, float *P, float *summary,
+                     void *ws, size_t ws_bytes, void *stream)
+{
+    const int rc = check_desc(desc);
+    if (rc != ZEDA_OK) return rc;
+    if (desc->T > 0 && (!x || !topk_ids || !topk_gates || !probs)) return ZEDA_EINVAL;
+    if (!w_router || !counts || !P || !summary || !ws || !(w > 0.f)) return ZEDA_EINVAL;
+    if (!aligned16(x) || !aligned16(w_router) || !aligned16(topk_ids) || !aligned16(topk_gates) || !aligned16(probs) || !aligned16(ws) ||
+        (router_bias && !aligned16(router_bias)) || !aligned4(counts) || !aligned4(P) || !aligned4(summary))
+        return ZEDA_EINVAL;
+    if (ws_bytes < route_train_ws_bytes(desc)) return ZEDA_EWORKSPACE;
+    return launch_route_train(desc, x, w_router, router_bias, token_mask, alpha, w, topk_ids, topk_gates, probs, counts, P, summary, ws,
+                              (hipStream_t)stream);
+}
+
+size_t zeda_route_backward_workspace_bytes(const zeda_layer_desc *desc) { return check_desc(desc) == ZEDA_OK ? route_backward_ws_bytes(desc) : 0; }
+
+int zeda_route_backward(const zeda_layer_desc *desc, const void *x, const void *w_router, const float *probs, const int32_t *topk_ids,
+                        const float *topk_gates, const uint8_t *token_mask, const int32_t *counts, float alpha, float w, const float *d_loss,
+                        const float *d_gates, void *dx, float *dw_router, float *dbias, void *ws, size_t ws_bytes, void *stream)
+{
+    const int rc = check_desc(desc);
+    if (rc != ZEDA_OK) return rc;
+    if (desc->T > 0 && (!x || !probs || !topk_ids || !topk_gates)) return ZEDA_EINVAL;
+    if (!w_router || !counts || !ws || !(w > 0.f)) return ZEDA_EINVAL;
+    if ((!d_loss && !d_gates) || (!dx && !dw_router && !dbias)) return ZEDA_EINVAL;  // nothing comes in, or nothing goes out
+    if (!aligned16(x) || !aligned16(w_router) || !aligned16(probs) || !aligned16(topk_ids) || !aligned16(topk_gates) || !aligned4(counts) ||
+        !aligned4(d_loss) || !aligned16(d_gates) || !aligned16(dx) || !aligned16(dw_router) || !aligned4(dbias) || !aligned16(ws))
+        return ZEDA_EINVAL;
+    const size_t NE = (size_t)desc->N + desc->Z, nx = (size_t)desc->T * desc->H * elt_size(desc), nw = NE * desc->H;
+    if (overlap(dx, nx, x, nx) || overlap(dx, nx, w_router, nw * elt_size(desc)) || overlap(dw_router, nw * 4, x, nx) ||
+        overlap(dw_router, nw * 4, w_router, nw * elt_size(desc)))
+        return ZEDA_EINVAL;
+    if (ws_bytes < route_backward_ws_bytes(desc)) return ZEDA_EWORKSPACE;
+    return launch_route_backward(desc, x, w_router, probs, topk_ids, topk_gates, token_mask, counts, alpha, w, d_loss, d_gates, dx, dw_router,
+                                 dbias, ws, (hipStream_t)stream);
+}
+
+int zeda_combine_backward(const zeda_layer_desc *desc, const void *d_out, const void *y_slot, const int32_t *topk_ids, const float *topk_gates,
+                          const int32_t *slot_to_row, const void *x, float *d_gates, void *d_y_slot, void *dx, void *stream)
+{
+    const int rc = check_desc(desc);
+    if (rc != ZEDA_OK) return rc;
+    if (desc->T == 0) return ZEDA_OK;
+    const bool copy = desc->free_expert == ZEDA_EXPERT_COPY;
+    if (!d_out || !y_slot || !topk_ids || !topk_gates || !slot_to_row || !d_gates || (copy && !x) || (!copy && dx)) return ZEDA_EINVAL;
+    if (!aligned16(d_out) || !aligned16(y_slot) || !aligned16(topk_ids) || !aligned16(topk_gates) || !aligned16(slot_to_row) ||
+        !aligned16(d_gates) || !aligned16(d_y_slot) || !aligned16(dx) || (copy && !aligned16(x)))
+        return ZEDA_EINVAL;
+    const size_t row = (size_t)desc->H * elt_size(desc), ny = (size_t)desc->T * desc->K * row, nx = (size_t)desc->T * row;
+    if (overlap(d_y_slot, ny, y_slot, ny) || overlap(d_y_slot, ny, d_out, nx) || overlap(dx, nx, d_out, nx) || overlap(dx, nx, y_slot, ny) ||
+        overlap(dx, nx, d_y_slot, ny) || (copy && (overlap(dx, nx, x, nx) || overlap(d_y_slot, ny, x, nx))))
+        return ZEDA_EINVAL;
+    return launch_combine_backward(desc, d_out, y_slot, topk_ids, topk_gates, slot_to_row, x, d_gates, d_y_slot, dx, (hipStream_t)stream);
+}
+
 int zeda_token_zero_slots(const zeda_layer_desc *desc, const int32_t *topk_ids, int32_t *zero_slots, int accumulate,
                           void *stream)
 {

@@ -54,6 +54,14 @@ bool dispatch_counts_supported(const zeda_layer_desc *d);
 int launch_dispatch_counts(const zeda_layer_desc *d, const int32_t *ids, const uint8_t *cnt8, int32_t *offsets,
                            int32_t *sorted_slot, int32_t *slot_to_row, int32_t *num_real, int32_t *num_real_copy,
                            hipStream_t s);
+// Only the logits, without biases: `slices` tables [Tpad][E] over slices of the hidden dimension, added in order (a training step
+// selects from them and keeps the probabilities).
+struct RouteTables {
+    int slices, Tpad, E;
+    size_t bytes() const { return (size_t)slices * Tpad * E * sizeof(float); }
+};
+RouteTables route_tables(const zeda_layer_desc *d);
+int launch_route_tables(const zeda_layer_desc *d, const void *x, const void *wr, float *tables, hipStream_t s);
 // Section 2.2 statistics over the batch of all T tokens (f, P: [N+Z]; summary: 7 floats); ws of routing_stats_ws_bytes
 int launch_routing_stats(const zeda_layer_desc *d, const void *x, const void *wr, const float *bias, float alpha, float w,
                          float *f, float *P, float *summary, void *ws, hipStream_t s);
@@ -99,6 +107,17 @@ bool combine_block_supported(const zeda_layer_desc *d);
 int launch_combine_block(const zeda_layer_desc *d, const void *y_slot, const int16_t *y_exp, const int32_t *ids, const float *gates,
                          const int32_t *slot_to_row, const void *x, void *x_res, const void *gamma, float eps,
                          void *xn_next, hipStream_t s);
+
+// training: see zeda_route_train, zeda_route_backward, zeda_combine_backward
+size_t route_train_ws_bytes(const zeda_layer_desc *d);
+int launch_route_train(const zeda_layer_desc *d, const void *x, const void *wr, const float *bias, const uint8_t *mask, float alpha, float w,
+                       int32_t *ids, float *gates, float *probs, int32_t *counts, float *P, float *summary, void *ws, hipStream_t s);
+size_t route_backward_ws_bytes(const zeda_layer_desc *d);
+int launch_route_backward(const zeda_layer_desc *d, const void *x, const void *wr, const float *probs, const int32_t *ids, const float *gates,
+                          const uint8_t *mask, const int32_t *counts, float alpha, float w, const float *d_loss, const float *d_gates, void *dx,
+                          float *dw, float *dbias, void *ws, hipStream_t s);
+int launch_combine_backward(const zeda_layer_desc *d, const void *d_out, const void *y_slot, const int32_t *ids, const float *gates,
+                            const int32_t *slot_to_row, const void *x, float *d_gates, void *d_y_slot, void *dx, hipStream_t s);
 
 inline int last_launch_status() { return hipGetLastError() == hipSuccess ? ZEDA_OK : ZEDA_EHIP; }
 

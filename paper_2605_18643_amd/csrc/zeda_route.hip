@@ -429,6 +429,7 @@ struct RouteExtras {
     float *p_part;
     PlaceOut place;
     TilePlace *tp;  // given: the gate/up kernel selects
+    bool tables;    // only the logit tables, for a selection of the caller's
 };
 
 template <int NB, int TB, int W>
@@ -447,7 +448,7 @@ static int launch_route_bf16(const zeda_layer_desc *d, const void *x, const void
     }
     const int NE = d->N + d->Z, Tpad = route_tpad(d);
     route_bf16_kernel<NB, TB, W><<<dim3(ceil_div(d->T, C::TOK), slices), C::THREADS, C::LDS_BYTES, s>>>(
-        (const bf16_t *)x, (const bf16_t *)wr, bias, d->T, d->H, d->N, NE, d->K, d->gate_norm, ids, gates, slices > 1 ? partial : nullptr, Tpad,
+        (const bf16_t *)x, (const bf16_t *)wr, bias, d->T, d->H, d->N, NE, d->K, d->gate_norm, ids, gates, slices > 1 || ex.tables ? partial : nullptr, Tpad,
         ex.cnt8, ex.cnt_ld, ex.p_part);
     if (ex.tp && slices > 1) {
         ex.tp->partial = partial;
@@ -457,6 +458,7 @@ static int launch_route_bf16(const zeda_layer_desc *d, const void *x, const void
         ex.tp->by_rows = W == kRouteWavesSmall;
         return last_launch_status();
     }
+    if (ex.tables) return last_launch_status();
     const dim3 sgrid(ceil_div(d->T, kSelectTokens));
 #define ZEDA_SELECT(NP) route_select_kernel<NB, NP, W><<<sgrid, C::THREADS, 0, s>>>(partial, Tpad, bias, d->T, d->N, NE, d->K, d->gate_norm, ids, gates, ex.cnt8, ex.cnt_ld, ex.p_part, ex.place)
     if (slices == 2) ZEDA_SELECT(2);
@@ -781,7 +783,7 @@ int launch_routing_stats(const zeda_layer_desc *d, const void *x, const void *wr
         float *partial = route_ws_bytes(d) ? (float *)ws : nullptr;
         uint8_t *cnt8 = (uint8_t *)ws + align_up(route_ws_bytes(d), 256);
         float *p_part = (float *)(cnt8 + route_counts_bytes(d));
-        const RouteExtras ex = {cnt8, route_counts_ld(d), p_part, {}, nullptr};
+        const RouteExtras ex = {cnt8, route_counts_ld(d), p_part, {}, nullptr, false};
         const RoutePlan plan = route_plan(d, partial != nullptr);
         const int prows = ceil_div(d->T, plan.slices > 1 ? kSelectTokens : 16 * plan.tb);  // workgroups that select
         const int rc = launch_route_bf16_any(d, x, wr, bias, nullptr, nullptr, partial, ex, s);
@@ -812,11 +814,25 @@ int launch_routing_stats(const zeda_layer_desc *d, const void *x, const void *wr
     return last_launch_status();
 }
 
+// The logits without their biases, as tables [slices][Tpad][E] over slices of the hidden dimension to be added in order: the sums of
+// zeda_route with scratch.
+RouteTables route_tables(const zeda_layer_desc *d)
+{
+    const int E = ceil_div(d->N + d->Z, 32) * 32;
+    return {d->dtype == ZEDA_BF16 ? route_plan(d, true).slices : 1, route_tpad(d), E};
+}
+int launch_route_tables(const zeda_layer_desc *d, const void *x, const void *wr, float *tables, hipStream_t s)
+{
+    if (d->dtype != ZEDA_BF16) return launch_route_f32(d, x, wr, nullptr, nullptr, nullptr, tables, route_tables(d).E, s);
+    const RouteExtras ex = {nullptr, 0, nullptr, {}, nullptr, true};
+    return launch_route_bf16_any(d, x, wr, nullptr, nullptr, nullptr, tables, ex, s);
+}
+
 int launch_route(const zeda_layer_desc *d, const void *x, const void *wr, const float *bias, int32_t *ids, float *gates,
                  float *partial, uint8_t *cnt8, const PlaceOut *place, TilePlace *tp, hipStream_t s)
 {
     if (d->dtype == ZEDA_BF16) {
-        const RouteExtras ex = {cnt8, cnt8 ? route_counts_ld(d) : 0, nullptr, place ? *place : PlaceOut{}, tp};
+        const RouteExtras ex = {cnt8, cnt8 ? route_counts_ld(d) : 0, nullptr, place ? *place : PlaceOut{}, tp, false};
         return launch_route_bf16_any(d, x, wr, bias, ids, gates, partial, ex, s);
     }
     return launch_route_f32(d, x, wr, bias, ids, gates, nullptr, 0, s);

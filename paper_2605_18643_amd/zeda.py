@@ -30,7 +30,9 @@ EXPORTS = ("zeda_status_string", "zeda_workspace_bytes", "zeda_route_workspace_b
            "zeda_init_zero_expert_rows", "zeda_stream_read_probe", "zeda_mfma_probe", "zeda_token_zero_slots", "zeda_overlap_probe",
            "zeda_quantize_rows_fp8", "zeda_quantize_weights_fp8", "zeda_fp8_expert_bytes", "zeda_pack_expert_weights_fp8",
            "zeda_expert_ffn_workspace_bytes_fp8", "zeda_workspace_bytes_fp8", "zeda_workspace_layout_fp8", "zeda_expert_ffn_fp8",
-           "zeda_moe_forward_fp8", "zeda_moe_block_forward_fp8")
+           "zeda_moe_forward_fp8", "zeda_moe_block_forward_fp8",
+           "zeda_route_train_workspace_bytes", "zeda_route_train", "zeda_route_backward_workspace_bytes", "zeda_route_backward",
+           "zeda_combine_backward")
 
 
 class LayerDesc(ctypes.Structure):
@@ -125,7 +127,8 @@ def lib() -> ctypes.CDLL:
         L.zeda_fp8_expert_bytes.argtypes = [dp, ctypes.POINTER(sz)]
         L.zeda_pack_expert_weights_fp8.restype = i32
         L.zeda_pack_expert_weights_fp8.argtypes = [dp, vp, vp, vp, vp, vp, vp, ep, vp]
-        for name in ("zeda_expert_ffn_workspace_bytes_fp8", "zeda_workspace_bytes_fp8"):
+        for name in ("zeda_expert_ffn_workspace_bytes_fp8", "zeda_workspace_bytes_fp8", "zeda_route_train_workspace_bytes",
+                     "zeda_route_backward_workspace_bytes"):
             getattr(L, name).restype = sz
             getattr(L, name).argtypes = [dp]
         L.zeda_workspace_layout_fp8.restype = i32
@@ -136,6 +139,13 @@ def lib() -> ctypes.CDLL:
         L.zeda_moe_forward_fp8.argtypes = [dp, vp, vp, vp, ep, vp, vp, vp, sz, vp]
         L.zeda_moe_block_forward_fp8.restype = i32
         L.zeda_moe_block_forward_fp8.argtypes = [dp, vp, vp, vp, vp, ep, vp, ctypes.c_float, vp, vp, vp, sz, vp]
+        fl = ctypes.c_float
+        L.zeda_route_train.restype = i32
+        L.zeda_route_train.argtypes = [dp, vp, vp, vp, vp, fl, fl, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.zeda_route_backward.restype = i32
+        L.zeda_route_backward.argtypes = [dp, vp, vp, vp, vp, vp, vp, vp, fl, fl, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.zeda_combine_backward.restype = i32
+        L.zeda_combine_backward.argtypes = [dp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
         _lib = L
     return _lib
 
@@ -410,6 +420,37 @@ def zeda_moe_block_forward_fp8(desc, xn, x_res, w_router, router_bias, experts: 
     _check(lib().zeda_moe_block_forward_fp8(ctypes.byref(desc), _ptr(xn), _ptr(x_res), _ptr(w_router), _ptr(router_bias), ctypes.byref(experts),
                                             _ptr(gamma_next), float(eps), _ptr(xn_next), _ptr(num_real_out), _ptr(ws),
                                             ws.numel() * ws.element_size(), _stream(stream)), "zeda_moe_block_forward_fp8")
+
+
+def route_train_workspace_bytes(desc: LayerDesc) -> int:
+    return int(lib().zeda_route_train_workspace_bytes(ctypes.byref(desc)))
+
+
+def route_backward_workspace_bytes(desc: LayerDesc) -> int:
+    return int(lib().zeda_route_backward_workspace_bytes(ctypes.byref(desc)))
+
+
+def zeda_route_train(desc, x, w_router, router_bias, token_mask, alpha: float, w: float, topk_ids, topk_gates, probs, counts, mean_probs, summary,
+                     ws, stream=None) -> None:
+    """zeda_route that also leaves probs[T, N+Z], and over the tokens with token_mask (uint8[T] or None) != 0 counts[N+Z], mean_probs[N+Z] and
+    summary[7] (as zeda_routing_stats: the balance losses are summary[5] and summary[6])."""
+    _check(lib().zeda_route_train(ctypes.byref(desc), _ptr(x), _ptr(w_router), _ptr(router_bias), _ptr(token_mask), float(alpha), float(w),
+                                  _ptr(topk_ids), _ptr(topk_gates), _ptr(probs), _ptr(counts), _ptr(mean_probs), _ptr(summary), _ptr(ws),
+                                  ws.numel() * ws.element_size(), _stream(stream)), "zeda_route_train")
+
+
+def zeda_route_backward(desc, x, w_router, probs, topk_ids, topk_gates, token_mask, counts, alpha: float, w: float, d_loss, d_gates, dx, dw_router,
+                        dbias, ws, stream=None) -> None:
+    """Gradients of d_loss[0] L_A + d_loss[1] L_GA + <d_gates, topk_gates>: dx (type of x), dw_router and dbias (fp32); each may be None."""
+    _check(lib().zeda_route_backward(ctypes.byref(desc), _ptr(x), _ptr(w_router), _ptr(probs), _ptr(topk_ids), _ptr(topk_gates), _ptr(token_mask),
+                                     _ptr(counts), float(alpha), float(w), _ptr(d_loss), _ptr(d_gates), _ptr(dx), _ptr(dw_router), _ptr(dbias),
+                                     _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)), "zeda_route_backward")
+
+
+def zeda_combine_backward(desc, d_out, y_slot, topk_ids, topk_gates, slot_to_row, x, d_gates, d_y_slot, dx, stream=None) -> None:
+    """Backward of zeda_combine.  d_y_slot may be None; x and dx belong to EXPERT_COPY (None otherwise, dx None if not wanted)."""
+    _check(lib().zeda_combine_backward(ctypes.byref(desc), _ptr(d_out), _ptr(y_slot), _ptr(topk_ids), _ptr(topk_gates), _ptr(slot_to_row), _ptr(x),
+                                       _ptr(d_gates), _ptr(d_y_slot), _ptr(dx), _stream(stream)), "zeda_combine_backward")
 
 
 def ws_views(desc: LayerDesc, ws: torch.Tensor):
