@@ -6,7 +6,7 @@
 
 #include <type_traits>
 
-#include "zeda_internal.h"
+#include "zeda_place.h"
 #include "zeda_select.h"
 
 namespace zeda {
@@ -23,7 +23,8 @@ template <int NB>
 __global__ __launch_bounds__(256) void train_select_kernel(const float *__restrict__ tables, int slices, int Tpad,
                                                            const float *__restrict__ bias, const uint8_t *__restrict__ mask, int T, int N,
                                                            int NE, int K, int gate_norm, int32_t *__restrict__ ids, float *__restrict__ gates,
-                                                           float *__restrict__ probs, float *__restrict__ part_p, int32_t *__restrict__ part_c)
+                                                           float *__restrict__ probs, float *__restrict__ part_p, int32_t *__restrict__ part_c,
+                                                           int32_t *__restrict__ done)
 {
     constexpr int E = NB * 32, LD = E + 1;
     __shared__ float lg[kTrainTokens * LD];
@@ -55,61 +56,94 @@ __global__ __launch_bounds__(256) void train_select_kernel(const float *__restri
         int n = 0;
         for (int tk = 0; tk < kTrainTokens; ++tk) n += s_on[tk];
         part_c[(size_t)blockIdx.x * (NE + 1) + NE] = n;
+        if (blockIdx.x == 0) *done = 0;
     }
 }
 
-// The batch sums and the losses, by one workgroup; sums over blocks in 64 bits and in a fixed order.
-constexpr int kTrainFinalThreads = 1024;
-__global__ __launch_bounds__(kTrainFinalThreads) void train_final_kernel(const float *__restrict__ part_p, const int32_t *__restrict__ part_c, int nblk,
-                                                                         int N, int NE, int K, float alpha, float w, int32_t *__restrict__ counts,
-                                                                         float *__restrict__ P, float *__restrict__ summary)
+// The batch sums: a workgroup adds up kFinalExperts experts' partial sums (in 64 bits and in a fixed order), and the last one to
+// finish, found by a counter that train_select_kernel has cleared, does the losses.  One workgroup for everything took 34 us at 8192
+// tokens and 160 experts (655 KB through one CU).
+constexpr int kFinalThreads = 1024, kFinalExperts = 8;
+__global__ __launch_bounds__(kFinalThreads) void train_final_kernel(const float *__restrict__ part_p, const int32_t *__restrict__ part_c, int nblk,
+                                                                    int N, int NE, int K, float alpha, float w, int32_t *counts, float *P,
+                                                                    float *__restrict__ summary, int32_t *__restrict__ done)
 {
-    __shared__ double s_p[kTrainFinalThreads];
-    __shared__ int s_c[kTrainFinalThreads], s_n[kTrainFinalThreads];
-    __shared__ double s_f[kMaxExperts], s_P[kMaxExperts];
-    const int tid = threadIdx.x, parts = kTrainFinalThreads / NE, e = tid % NE, part = tid / NE;
+    constexpr int PARTS = kFinalThreads / kFinalExperts, W = kFinalThreads / 64;
+    __shared__ double s_p[W][kFinalExperts];
+    __shared__ int s_c[W][kFinalExperts], s_n[W], s_last;
+    const int tid = threadIdx.x, wave = tid >> 6, e = blockIdx.x * kFinalExperts + tid % kFinalExperts;
     double p = 0.;
     int c = 0, n = 0;
-    if (part < parts)
-        for (int b = part; b < nblk; b += parts) {
+    if (e < NE) {
+#pragma unroll 4
+        for (int b = tid / kFinalExperts; b < nblk; b += PARTS) {
             p += (double)part_p[(size_t)b * NE + e];
             c += part_c[(size_t)b * (NE + 1) + e];
         }
-    for (int b = tid; b < nblk; b += kTrainFinalThreads) n += part_c[(size_t)b * (NE + 1) + NE];
-    s_p[tid] = p;
-    s_c[tid] = c;
-    s_n[tid] = n;
-    __syncthreads();
-    for (int h = kTrainFinalThreads / 2; h >= 1; h >>= 1) {
-        if (tid < h) s_n[tid] += s_n[tid + h];
-        __syncthreads();
     }
-    if (tid < NE) {
-        for (int q = 1; q < parts; ++q) { p += s_p[q * NE + tid]; c += s_c[q * NE + tid]; }
-        const double all = s_n[0] > 0 ? s_n[0] : 1;  // nothing counts: f = P = 0
-        s_f[tid] = c / all;
-        s_P[tid] = p / all;
-        counts[tid] = c;
-        P[tid] = (float)(p / all);
-    }
-    __syncthreads();
-    if (tid == 0) {
-        double fE = 0., PE = 0., fZ = 0., PZ = 0., fP = 0.;
-        for (int i = 0; i < NE; ++i) {
-            fP += s_f[i] * s_P[i];
-            (i < N ? fE : fZ) += s_f[i];
-            (i < N ? PE : PZ) += s_P[i];
+    for (int b = tid; b < nblk; b += kFinalThreads) n += part_c[(size_t)b * (NE + 1) + NE];
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) {
+        n += __shfl_xor(n, off);
+        if (off >= kFinalExperts) {
+            p += __shfl_xor(p, off);
+            c += __shfl_xor(c, off);
         }
-        const double Zw = (double)(NE - N) * w;
-        summary[0] = (float)fE; summary[1] = (float)PE; summary[2] = (float)fZ; summary[3] = (float)PZ;
-        summary[4] = (float)(fZ / K);
-        summary[5] = (float)((double)alpha * NE / K * fP);                                                  // Eq. 4
-        summary[6] = (float)((double)alpha * (N + Zw) / K * (fE * PE / N + (NE > N ? fZ * PZ / Zw : 0.)));  // Eq. 5-6
+    }
+    if ((tid & 63) < kFinalExperts) {
+        s_p[wave][tid & 63] = p;
+        s_c[wave][tid & 63] = c;
+        if ((tid & 63) == 0) s_n[wave] = n;
+    }
+    __syncthreads();
+    n = 0;
+#pragma unroll
+    for (int q = 0; q < W; ++q) n += s_n[q];
+    n = max(1, n);  // nothing counts: f = P = 0
+    if (tid < kFinalExperts && e < NE) {
+        p = 0.;
+        c = 0;
+#pragma unroll
+        for (int q = 0; q < W; ++q) { p += s_p[q][tid]; c += s_c[q][tid]; }
+        __hip_atomic_store(counts + e, c, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __hip_atomic_store(P + e, (float)(p / n), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    // (the stores above and this are one wave's: one release covers them)
+    if (tid == 0) s_last = __hip_atomic_fetch_add(done, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.x - 1;
+    __syncthreads();
+    if (!s_last) return;
+    double v[5] = {0., 0., 0., 0., 0.};  // f_E, P_E, f_Z, P_Z, sum of f P
+    if (tid < 64) {
+        for (int i = tid; i < NE; i += 64) {
+            const double f = (double)__hip_atomic_load(counts + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) / n;
+            const double q = (double)__hip_atomic_load(P + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            v[4] += f * q;
+            v[i < N ? 0 : 2] += f;
+            v[i < N ? 1 : 3] += q;
+        }
+#pragma unroll
+        for (int q = 0; q < 5; ++q)
+#pragma unroll
+            for (int off = 32; off >= 1; off >>= 1) v[q] += __shfl_xor(v[q], off);
+        if (tid == 0) {
+            const double Zw = (double)(NE - N) * w;
+            for (int q = 0; q < 4; ++q) summary[q] = (float)v[q];
+            summary[4] = (float)(v[2] / K);
+            summary[5] = (float)((double)alpha * NE / K * v[4]);                                                               // Eq. 4
+            summary[6] = (float)((double)alpha * (N + Zw) / K * (v[0] * v[1] / N + (NE > N ? v[2] * v[3] / Zw : 0.)));  // Eq. 5-6
+        }
     }
 }
 
+// no token: everything is zero
+__global__ __launch_bounds__(256) void train_nothing_kernel(int NE, int32_t *__restrict__ counts, float *__restrict__ P, float *__restrict__ summary)
+{
+    if (threadIdx.x < NE) { counts[threadIdx.x] = 0; P[threadIdx.x] = 0.f; }
+    if (threadIdx.x < 7) summary[threadIdx.x] = 0.f;
+}
+
 struct TrainWs {
-    size_t tables, part_p, part_c, total;
+    size_t tables, part_p, part_c, done, total;
 };
 static TrainWs train_ws(const zeda_layer_desc *d)
 {
@@ -120,6 +154,7 @@ static TrainWs train_ws(const zeda_layer_desc *d)
     w.tables = take(route_tables(d).bytes());
     w.part_p = take(nblk * NE * 4);
     w.part_c = take(nblk * (NE + 1) * 4);
+    w.done = take(4);
     w.total = o;
     return w;
 }
@@ -131,20 +166,22 @@ int launch_route_train(const zeda_layer_desc *d, const void *x, const void *wr, 
     const TrainWs L = train_ws(d);
     const RouteTables t = route_tables(d);
     float *tables = (float *)((char *)ws + L.tables), *part_p = (float *)((char *)ws + L.part_p);
-    int32_t *part_c = (int32_t *)((char *)ws + L.part_c);
+    int32_t *part_c = (int32_t *)((char *)ws + L.part_c), *done = (int32_t *)((char *)ws + L.done);
     const int NE = d->N + d->Z, nblk = ceil_div(d->T, kTrainTokens);
-    if (d->T > 0) {
-        const int rc = launch_route_tables(d, x, wr, tables, s);
-        if (rc != ZEDA_OK) return rc;
-#define ZEDA_TRAIN(NB) train_select_kernel<NB><<<nblk, 256, 0, s>>>(tables, t.slices, t.Tpad, bias, mask, d->T, d->N, NE, d->K, d->gate_norm, ids, gates, probs, part_p, part_c)
-        switch (t.E / 32) {
-            case 1: ZEDA_TRAIN(1); break; case 2: ZEDA_TRAIN(2); break; case 3: ZEDA_TRAIN(3); break; case 4: ZEDA_TRAIN(4); break;
-            case 5: ZEDA_TRAIN(5); break; case 6: ZEDA_TRAIN(6); break; case 7: ZEDA_TRAIN(7); break; default: ZEDA_TRAIN(8); break;
-        }
-#undef ZEDA_TRAIN
-        if (hipGetLastError() != hipSuccess) return ZEDA_EHIP;
+    if (d->T == 0) {
+        train_nothing_kernel<<<1, 256, 0, s>>>(NE, counts, P, summary);
+        return last_launch_status();
     }
-    train_final_kernel<<<1, kTrainFinalThreads, 0, s>>>(part_p, part_c, nblk, d->N, NE, d->K, alpha, w, counts, P, summary);
+    const int rc = launch_route_tables(d, x, wr, tables, s);
+    if (rc != ZEDA_OK) return rc;
+#define ZEDA_TRAIN(NB) train_select_kernel<NB><<<nblk, 256, 0, s>>>(tables, t.slices, t.Tpad, bias, mask, d->T, d->N, NE, d->K, d->gate_norm, ids, gates, probs, part_p, part_c, done)
+    switch (t.E / 32) {
+        case 1: ZEDA_TRAIN(1); break; case 2: ZEDA_TRAIN(2); break; case 3: ZEDA_TRAIN(3); break; case 4: ZEDA_TRAIN(4); break;
+        case 5: ZEDA_TRAIN(5); break; case 6: ZEDA_TRAIN(6); break; case 7: ZEDA_TRAIN(7); break; default: ZEDA_TRAIN(8); break;
+    }
+#undef ZEDA_TRAIN
+    if (hipGetLastError() != hipSuccess) return ZEDA_EHIP;
+    train_final_kernel<<<ceil_div(NE, kFinalExperts), kFinalThreads, 0, s>>>(part_p, part_c, nblk, d->N, NE, d->K, alpha, w, counts, P, summary, done);
     return last_launch_status();
 }
 
@@ -153,10 +190,10 @@ int launch_route_train(const zeda_layer_desc *d, const void *x, const void *wr, 
 // ---------------------------------------------------------------------------------------------------------------------
 // The gradient of the logits,
 //   dl_e = p_e (a_e - sum_j p_j a_j) + the gates' part,   a_e = (dL_A alpha (N+Z)/K f_e + dL_GA alpha (N + Z w)/K f_E/N or f_Z/(Z w)) / n,
-// does not change when a constant is added to a: the slopes' mean is taken off in 64 bits, so that the difference keeps what the
-// slopes differ by.  Gates: SOFTMAX adds dg_j to a at the selected experts; the normalised forms add g_j (dg_j - s), s = sum_l dg_l g_l,
+// does not change when a constant is added to a: the slopes' mean is taken off, in 64 bits, so that what they differ
+// by is kept.  Gates: SOFTMAX adds dg_j to a at the selected experts; the normalised forms add g_j (dg_j - s), s = sum_l dg_l g_l,
 // on the experts of the denominator and g_j dg_j on a selected expert outside it.
-constexpr int kBackTokens = 64;
+constexpr int kBackTokens = 32, kBackThreads = 512;
 
 // bf16 parts by truncation: v = v0 + v1 + v2 exactly (24 bits)
 __device__ __forceinline__ uint16_t top_bits(float v) { return (uint16_t)(__float_as_uint(v) >> 16); }
@@ -168,66 +205,74 @@ struct LogitGrad {
     const uint8_t *mask;
     int T, N, NE, K, gate_norm;
     float alpha, w;
-    void *rows, *cols;    // dl as [parts][Tp][NEp] and [parts][NEp][Tp]
+    // dl twice, as tiles in the order in which the products fetch them: rows [part][t / 16][e / 32][t % 16][e % 32] and
+    // cols [part][t / 32][e][t % 32]
+    void *rows, *cols;
     float *part_b;        // [blocks][NE]: sums over the block's tokens
+    uint32_t *on;         // [blocks]
     int Tp, NEp;
 };
 
-// A wave takes a token at a time, lane l the experts l, l + 64, ...  F32: both copies in fp32; else the rows as two bf16 parts (their
-// product is rounded to bf16), the columns as three (theirs stays fp32: nothing of dl is lost).
+// A wave takes four tokens, lane l the experts l, l + 64, ...  F32: both copies in fp32; else the rows as two bf16 parts (their
+// product is rounded to bf16), the columns as three (theirs stays fp32: nothing of dl is lost).  on[block]: which of the block's
+// tokens count, a bit each.
 template <bool F32>
-__global__ __launch_bounds__(256) void logit_grad_kernel(LogitGrad a)
+__global__ __launch_bounds__(kBackThreads) void logit_grad_kernel(LogitGrad a)
 {
+    constexpr int W = kBackThreads / 64, PER = kBackTokens / W;
     extern __shared__ float s_dl[];  // [kBackTokens][LD]
     __shared__ float s_a[kMaxExperts];
-    __shared__ double s_red[2][4];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, t0 = blockIdx.x * kBackTokens, NE = a.NE, N = a.N, LD = a.NEp + 1;
-    {
-        // slopes: thread e expert e
-        const double c = tid < NE ? (double)a.counts[tid] : 0.;
-        auto block_sum = [&](double v, int k) {
+    bool on[PER];
+    float p[PER][4], g[PER], dg[PER];
+    int id[PER];
 #pragma unroll
-            for (int off = 32; off >= 1; off >>= 1) v += __shfl_xor(v, off);
-            if (lane == 0) s_red[k][wave] = v;
-            __syncthreads();
-            const double r = (s_red[k][0] + s_red[k][1]) + (s_red[k][2] + s_red[k][3]);
-            __syncthreads();
-            return r;
-        };
-        const double cE = block_sum(tid < N ? c : 0., 0), cZ = block_sum(tid < N ? 0. : c, 1);
-        const double n = fmax(1., (cE + cZ) / a.K);
-        const double Zw = (double)(NE - N) * a.w, lA = a.d_loss ? (double)a.d_loss[0] : 0., lG = a.d_loss ? (double)a.d_loss[1] : 0.;
-        double v = tid < NE ? (double)a.alpha / a.K * (lA * NE * c + lG * (N + Zw) * (tid < N ? cE / N : cZ / Zw)) / n / n : 0.;
-        const double mean = block_sum(v, 0) / NE;
-        if (tid < NE) s_a[tid] = (float)(v - mean);
-        __syncthreads();
+    for (int k = 0; k < PER; ++k) {
+        const int t = t0 + wave * PER + k;
+        const size_t at = min(t, a.T - 1);
+        on[k] = t < a.T && (!a.mask || a.mask[at]);
+        id[k] = -1;
+        g[k] = dg[k] = 0.f;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) p[k][q] = lane + 64 * q < NE ? a.probs[at * NE + lane + 64 * q] : 0.f;
+        if (a.d_gates && lane < a.K) {
+            id[k] = a.ids[at * a.K + lane];
+            g[k] = a.gates[at * a.K + lane];
+            dg[k] = a.d_gates[at * a.K + lane];
+            if ((unsigned)id[k] >= (unsigned)NE) id[k] = -1, g[k] = dg[k] = 0.f;
+        }
     }
-    for (int k = wave; k < kBackTokens; k += 4) {
-        const int t = t0 + k;
-        const bool on = t < a.T && (!a.mask || a.mask[t]);
-        float dl[4] = {0.f, 0.f, 0.f, 0.f};
-        if (on) {
-            float p[4], u[4], g_of[4] = {}, v_of[4] = {};
+    if (wave == 0) {  // the slopes: lane l experts l, l + 64, ...
+        int c[4], cE = 0, cZ = 0;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int e = lane + 64 * q;
-                p[q] = e < NE ? a.probs[(size_t)t * NE + e] : 0.f;
-                u[q] = e < NE ? s_a[e] : 0.f;
-            }
-            float s = 0.f;
+        for (int q = 0; q < 4; ++q) {
+            const int e = lane + 64 * q;
+            c[q] = e < NE ? a.counts[e] : 0;
+            (e < N ? cE : cZ) += c[q];
+        }
+        cE = __builtin_amdgcn_readlane(wave_scan(cE), 63);
+        cZ = __builtin_amdgcn_readlane(wave_scan(cZ), 63);
+        const double n = fmax(1., (double)(cE + cZ) / a.K), Zw = (double)(NE - N) * a.w, unit = (double)a.alpha / a.K / (n * n);
+        const double kA = a.d_loss ? unit * a.d_loss[0] * NE : 0., kG = a.d_loss ? unit * a.d_loss[1] * (N + Zw) : 0.;
+        // without their mean: c_e - sum c / NE, and the groups' slopes share their difference
+        const double apart = NE > N ? kG * (cE * Zw - (double)cZ * N) / (N * Zw) / NE : 0.;
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            s_a[lane + 64 * q] = (float)(kA / NE * ((double)c[q] * NE - (cE + cZ)) + (lane + 64 * q < N ? apart * (NE - N) : -apart * N));
+    }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+        float dl[4] = {0.f, 0.f, 0.f, 0.f};
+        if (on[k]) {
+            float u[4], g_of[4] = {}, v_of[4] = {}, s = 0.f, pa = 0.f;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) u[q] = lane + 64 * q < NE ? s_a[lane + 64 * q] : 0.f;
             if (a.d_gates) {
-                int id = -1;
-                float g = 0.f, dg = 0.f;
-                if (lane < a.K) {
-                    id = a.ids[(size_t)t * a.K + lane];
-                    g = a.gates[(size_t)t * a.K + lane];
-                    dg = a.d_gates[(size_t)t * a.K + lane];
-                    if ((unsigned)id >= (unsigned)NE) id = -1, g = dg = 0.f;
-                }
                 for (int j = 0; j < a.K; ++j) {
-                    const int ej = __builtin_amdgcn_readlane(id, j);
-                    const float gj = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(g), j));
-                    const float dj = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(dg), j));
+                    const int ej = __builtin_amdgcn_readlane(id[k], j);
+                    const float gj = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(g[k]), j));
+                    const float dj = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(dg[k]), j));
                     s = fmaf(gj, dj, s);
 #pragma unroll
                     for (int q = 0; q < 4; ++q)
@@ -241,47 +286,56 @@ __global__ __launch_bounds__(256) void logit_grad_kernel(LogitGrad a)
                         }
                 }
             }
-            float pa = 0.f;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) pa = fmaf(p[q], u[q], pa);
+            for (int q = 0; q < 4; ++q) pa = fmaf(p[k][q], u[q], pa);
             pa = wave_sum(pa);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) dl[q] = lane + 64 * q < NE ? p[q] * (u[q] - pa) + (v_of[q] - s * g_of[q]) : 0.f;
+            for (int q = 0; q < 4; ++q) dl[q] = lane + 64 * q < NE ? p[k][q] * (u[q] - pa) + (v_of[q] - s * g_of[q]) : 0.f;
         }
 #pragma unroll
         for (int q = 0; q < 4; ++q)
-            if (lane + 64 * q < a.NEp) s_dl[k * LD + lane + 64 * q] = dl[q];
+            if (lane + 64 * q < a.NEp) s_dl[(wave * PER + k) * LD + lane + 64 * q] = dl[q];
     }
     __syncthreads();
     if (tid < NE) {
         double b = 0.;
+#pragma unroll 8
         for (int k = 0; k < kBackTokens; ++k) b += (double)s_dl[k * LD + tid];
         a.part_b[(size_t)blockIdx.x * NE + tid] = (float)b;
     }
-    const int Tp = a.Tp, NEp = a.NEp;
-    for (int i = tid; i < kBackTokens * NEp; i += 256) {
-        const int k = i / NEp, e = i - k * NEp;
-        const float v = s_dl[k * LD + e];
-        const size_t at = (size_t)(t0 + k) * NEp + e;
-        if (F32) {
-            ((float *)a.rows)[at] = v;
-        } else {
-            ((uint16_t *)a.rows)[at] = top_bits(v);
-            ((uint16_t *)a.rows)[(size_t)Tp * NEp + at] = top_bits(v - top_part(v));
-        }
+    if (wave == W - 1) {
+        const int t = t0 + lane;
+        const unsigned long long bits = __ballot(lane < kBackTokens && t < a.T && (!a.mask || a.mask[t]));
+        if (lane == 0) a.on[blockIdx.x] = (uint32_t)bits;
     }
-    for (int i = tid; i < kBackTokens * NEp; i += 256) {
-        const int e = i / kBackTokens, k = i - e * kBackTokens;
-        const float v = s_dl[k * LD + e];
-        const size_t at = (size_t)e * Tp + t0 + k;
+    const int Tp = a.Tp, NEp = a.NEp;
+    typedef uint16_t u16x4 __attribute__((ext_vector_type(4)));
+    const size_t plane = (size_t)Tp * NEp;
+    auto store = [&](void *to, size_t at, const float (&v)[4], int parts) {
         if (F32) {
-            ((float *)a.cols)[at] = v;
-        } else {
-            const float m = v - top_part(v);
-            ((uint16_t *)a.cols)[at] = top_bits(v);
-            ((uint16_t *)a.cols)[(size_t)Tp * NEp + at] = top_bits(m);
-            ((uint16_t *)a.cols)[(size_t)2 * Tp * NEp + at] = top_bits(m - top_part(m));
+            *reinterpret_cast<f32x4 *>((float *)to + at) = f32x4{v[0], v[1], v[2], v[3]};
+            return;
         }
+        float r[4] = {v[0], v[1], v[2], v[3]};
+        for (int q = 0; q < parts; ++q) {
+            u16x4 o;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                o[i] = top_bits(r[i]);
+                r[i] -= top_part(r[i]);
+            }
+            *reinterpret_cast<u16x4 *>((uint16_t *)to + q * plane + at) = o;
+        }
+    };
+    for (int i = tid; i < kBackTokens * NEp / 4; i += kBackThreads) {
+        const int k = i / (NEp / 4), e = (i - k * (NEp / 4)) * 4;
+        const float v[4] = {s_dl[k * LD + e], s_dl[k * LD + e + 1], s_dl[k * LD + e + 2], s_dl[k * LD + e + 3]};
+        store(a.rows, ((size_t)((t0 + k) >> 4) * (NEp >> 5) + (e >> 5)) * 512 + (k & 15) * 32 + (e & 31), v, 2);
+    }
+    for (int i = tid; i < kBackTokens * NEp / 4; i += kBackThreads) {
+        const int e = i / (kBackTokens / 4), k = (i - e * (kBackTokens / 4)) * 4;
+        const float v[4] = {s_dl[k * LD + e], s_dl[(k + 1) * LD + e], s_dl[(k + 2) * LD + e], s_dl[(k + 3) * LD + e]};
+        store(a.cols, ((size_t)(t0 >> 5) * NEp + e) * 32 + k, v, 3);
     }
 }
 
@@ -323,23 +377,27 @@ __global__ __launch_bounds__(256) void router_dx_bf16_kernel(const uint16_t *__r
         }
         turn8x4(r, wf[k]);
     }
-    constexpr int NEp = KS * 32;
-    for (int t0 = blockIdx.x * kDxTokens; t0 < min(T, (int)(blockIdx.x + 1) * kDxTokens); t0 += 16) {
-        f32x4 acc[4];
-#pragma unroll
-        for (int c = 0; c < 4; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
-        bf16x8 df[2][KS];
+    const int tb = min(T, (int)(blockIdx.x + 1) * kDxTokens);
+    const size_t plane = (size_t)Tp * KS * 32;
+    bf16x8 df[2][KS];
+    auto fetch = [&](int t0) {
 #pragma unroll
         for (int q = 0; q < 2; ++q)
 #pragma unroll
-            for (int k = 0; k < KS; ++k)
-                df[q][k] = *reinterpret_cast<const bf16x8 *>(dl + ((size_t)q * Tp + t0 + l16) * NEp + 32 * k + 8 * kq);
+            for (int k = 0; k < KS; ++k) df[q][k] = *reinterpret_cast<const bf16x8 *>(dl + q * plane + ((size_t)(t0 >> 4) * KS + k) * 512 + l16 * 32 + 8 * kq);
+    };
+    fetch(blockIdx.x * kDxTokens);
+    for (int t0 = blockIdx.x * kDxTokens; t0 < tb; t0 += 16) {
+        f32x4 acc[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int q = 1; q >= 0; --q)
 #pragma unroll
             for (int k = 0; k < KS; ++k)
 #pragma unroll
                 for (int c = 0; c < 4; ++c) acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(df[q][k], wf[k][c], acc[c], 0, 0, 0);
+        if (t0 + 16 < tb) fetch(t0 + 16);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int t = t0 + 4 * kq + i;
@@ -357,7 +415,7 @@ __global__ __launch_bounds__(256) void router_dx_f32_kernel(const float *__restr
                                                             float *__restrict__ dx)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, kq = lane >> 4;
-    const int h0 = (blockIdx.y * 4 + wave) * 64, t0 = blockIdx.x * kBackTokens, h = h0 + 4 * l16;
+    const int h0 = (blockIdx.y * 4 + wave) * 64, t0 = blockIdx.x * 64, h = h0 + 4 * l16;
     if (h0 >= H) return;
     f32x4 acc[4][4];  // [token block][column operand]
 #pragma unroll
@@ -370,7 +428,7 @@ __global__ __launch_bounds__(256) void router_dx_f32_kernel(const float *__restr
         for (int i = 0; i < 4; ++i) {
             const int e = e0 + 4 * kq + i;
             wf[i] = e < NE && h < H ? *reinterpret_cast<const f32x4 *>(wr + (size_t)e * H + h) : f32x4{0.f, 0.f, 0.f, 0.f};
-            df[i] = *reinterpret_cast<const f32x4 *>(dl + (size_t)(t0 + 16 * i + l16) * NEp + e0 + 4 * kq);
+            df[i] = *reinterpret_cast<const f32x4 *>(dl + ((size_t)(t0 / 16 + i) * (NEp >> 5) + (e0 >> 5)) * 512 + l16 * 32 + (e0 & 31) + 4 * kq);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -388,30 +446,32 @@ __global__ __launch_bounds__(256) void router_dx_f32_kernel(const float *__restr
         }
 }
 
-// dw_router[NE, H] = dl^T x, split over the tokens: part[split][NE16][H], added up by reduce_dw_kernel.  A wave has 64 columns and EB
-// blocks of 16 experts.  Rows of tokens that do not count are taken as zero whatever they hold.
+// dw_router[NE, H] = dl^T x, split over the tokens: part[split][NE16][H], added up by reduce_dw_kernel.  A workgroup has 128 columns,
+// EB blocks of 16 experts and a range of tokens; of its eight waves four share 64 columns and take 32 tokens (fp32: 16) in turn,
+// and their sums meet in LDS.  Rows of tokens that do not count are taken as zero whatever they hold.
+constexpr int kDwThreads = 512, kDwTurns = 4, kDwMaxBlocks = 6;
 template <int EB, bool F32>
-__global__ __launch_bounds__(256) void router_dw_kernel(const void *__restrict__ dlT, const void *__restrict__ xv, const uint8_t *__restrict__ mask, int T,
-                                                        int H, int Tp, int NEp, int per, float *__restrict__ part, int NE16)
+__global__ __launch_bounds__(kDwThreads) void router_dw_kernel(const void *__restrict__ dlT, const void *__restrict__ xv, const uint32_t *__restrict__ on,
+                                                               int H, int Tp, int NEp, int per, float *__restrict__ part, int NE16)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, kq = lane >> 4;
-    const int h0 = (blockIdx.x * 4 + wave) * 64, h = h0 + 4 * l16, e0 = blockIdx.z * EB * 16, ta = blockIdx.y * per, tb = min(ta + per, T);
-    if (h0 >= H) return;
+    __shared__ f32x4 s_sum[2][kDwTurns][16][32];  // [buffer][turn][expert][column / 4]
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, kq = lane >> 4;
+    const int turn = wave >> 1, h0 = blockIdx.x * 128, h = h0 + (wave & 1) * 64 + 4 * l16, e0 = blockIdx.z * EB * 16, ta = blockIdx.y * per, tb = min(ta + per, Tp);
     f32x4 acc[EB][4];
 #pragma unroll
     for (int b = 0; b < EB; ++b)
 #pragma unroll
         for (int c = 0; c < 4; ++c) acc[b][c] = f32x4{0.f, 0.f, 0.f, 0.f};
-    auto counts = [&](int t) { return t < T && (!mask || mask[t]); };
     if constexpr (F32) {
         const float *x = (const float *)xv, *dl = (const float *)dlT;
-        for (int t = ta; t < tb; t += 16) {
+        for (int t = ta + 16 * turn; t < tb; t += 16 * kDwTurns) {
+            const uint32_t bits = on[t >> 5] >> (t & 31);
             f32x4 xf[4], df[EB];
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                xf[i] = h < H && counts(t + 4 * kq + i) ? *reinterpret_cast<const f32x4 *>(x + (size_t)(t + 4 * kq + i) * H + h) : f32x4{0.f, 0.f, 0.f, 0.f};
+                xf[i] = h < H && (bits >> (4 * kq + i) & 1) ? *reinterpret_cast<const f32x4 *>(x + (size_t)(t + 4 * kq + i) * H + h) : f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int b = 0; b < EB; ++b) df[b] = *reinterpret_cast<const f32x4 *>(dl + (size_t)min(e0 + 16 * b + l16, NEp - 1) * Tp + t + 4 * kq);
+            for (int b = 0; b < EB; ++b) df[b] = *reinterpret_cast<const f32x4 *>(dl + ((size_t)(t >> 5) * NEp + min(e0 + 16 * b + l16, NEp - 1)) * 32 + (t & 31) + 4 * kq);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
 #pragma unroll
@@ -422,81 +482,111 @@ __global__ __launch_bounds__(256) void router_dw_kernel(const void *__restrict__
     } else {
         const bf16_t *x = (const bf16_t *)xv;
         const uint16_t *dl = (const uint16_t *)dlT;
-        for (int t = ta; t < tb; t += 32) {
-            uint2 r[8];
+        const size_t plane = (size_t)NEp * Tp;
+        uint2 r[8];
+        bf16x8 df[3][EB];
+        auto load_x = [&](int t) {
+            const uint32_t bits = on[t >> 5] >> (8 * kq);
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                r[i] = counts(t + 8 * kq + i) ? *reinterpret_cast<const uint2 *>(x + (size_t)(t + 8 * kq + i) * H + h) : make_uint2(0, 0);
+                r[i] = bits >> i & 1 ? *reinterpret_cast<const uint2 *>(x + (size_t)(t + 8 * kq + i) * H + h) : make_uint2(0, 0);
+        };
+        auto load_dl = [&](int q, int t) {
+#pragma unroll
+            for (int b = 0; b < EB; ++b)
+                df[q][b] = *reinterpret_cast<const bf16x8 *>(dl + q * plane + ((size_t)(t >> 5) * NEp + min(e0 + 16 * b + l16, NEp - 1)) * 32 + 8 * kq);
+        };
+        int t = ta + 32 * turn;
+        if (t < tb) {
+            load_x(t);
+#pragma unroll
+            for (int q = 2; q >= 0; --q) load_dl(q, t);
+        }
+        for (; t < tb; t += 32 * kDwTurns) {  // a part's registers are filled again as soon as its products are issued
+            const bool more = t + 32 * kDwTurns < tb;
             bf16x8 xf[4];
             turn8x4(r, xf);
+            if (more) load_x(t + 32 * kDwTurns);
 #pragma unroll
             for (int q = 2; q >= 0; --q) {
-                bf16x8 df[EB];
-#pragma unroll
-                for (int b = 0; b < EB; ++b)
-                    df[b] = *reinterpret_cast<const bf16x8 *>(dl + ((size_t)q * NEp + min(e0 + 16 * b + l16, NEp - 1)) * Tp + t + 8 * kq);
 #pragma unroll
                 for (int b = 0; b < EB; ++b)
 #pragma unroll
-                    for (int c = 0; c < 4; ++c) acc[b][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(df[b], xf[c], acc[b][c], 0, 0, 0);
+                    for (int c = 0; c < 4; ++c) acc[b][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(df[q][b], xf[c], acc[b][c], 0, 0, 0);
+                if (more) load_dl(q, t + 32 * kDwTurns);
             }
         }
     }
 #pragma unroll
-    for (int b = 0; b < EB; ++b)
+    for (int b = 0; b < EB; ++b) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int e = e0 + 16 * b + 4 * kq + i;
-            if (e < NE16 && h < H)
-                *reinterpret_cast<f32x4 *>(part + ((size_t)blockIdx.y * NE16 + e) * H + h) = f32x4{acc[b][0][i], acc[b][1][i], acc[b][2][i], acc[b][3][i]};
-        }
+        for (int i = 0; i < 4; ++i)
+            s_sum[b & 1][turn][4 * kq + i][(wave & 1) * 16 + l16] = f32x4{acc[b][0][i], acc[b][1][i], acc[b][2][i], acc[b][3][i]};
+        __syncthreads();
+        const int row = threadIdx.x >> 5, q = threadIdx.x & 31, e = e0 + 16 * b + row;
+        if (e < NE16 && h0 + 4 * q < H)
+            *reinterpret_cast<f32x4 *>(part + ((size_t)blockIdx.y * NE16 + e) * H + h0 + 4 * q) =
+                (s_sum[b & 1][0][row][q] + s_sum[b & 1][1][row][q]) + (s_sum[b & 1][2][row][q] + s_sum[b & 1][3][row][q]);
+    }
 }
 
-// dw = the splits' sums, dbias = the token blocks' sums (last workgroup); in a fixed order
-__global__ __launch_bounds__(256) void reduce_dw_kernel(const float *__restrict__ part, int splits, int NE, int NE16, int H, float *__restrict__ dw,
+// dw = the splits' sums; dbias = the token blocks' sums, eight experts to each of the last workgroups.  In a fixed order.
+constexpr int kBiasExperts = 8;
+__global__ __launch_bounds__(256) void reduce_dw_kernel(const float *__restrict__ part, int splits, int NE, int NE16, int H, int nw, float *__restrict__ dw,
                                                         const float *__restrict__ part_b, int nblk, float *__restrict__ dbias)
 {
-    if (blockIdx.x == gridDim.x - 1) {
-        if (dbias && threadIdx.x < NE) {
-            double b = 0.;
-            for (int k = 0; k < nblk; ++k) b += (double)part_b[(size_t)k * NE + threadIdx.x];
-            dbias[threadIdx.x] = (float)b;
+    if ((int)blockIdx.x >= nw) {
+        __shared__ double s_b[256];
+        const int e = (blockIdx.x - nw) * kBiasExperts + threadIdx.x % kBiasExperts;
+        double b = 0.;
+        if (e < NE) {
+#pragma unroll 4
+            for (int k = threadIdx.x / kBiasExperts; k < nblk; k += 256 / kBiasExperts) b += (double)part_b[(size_t)k * NE + e];
+        }
+        s_b[threadIdx.x] = b;
+        __syncthreads();
+        if (threadIdx.x < kBiasExperts && e < NE) {
+            for (int k = 1; k < 256 / kBiasExperts; ++k) b += s_b[k * kBiasExperts + threadIdx.x];
+            dbias[e] = (float)b;
         }
         return;
     }
     const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
-    if (!dw || i >= (size_t)NE * H) return;
+    if (i >= (size_t)NE * H) return;
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
     for (int q = 0; q < splits; ++q) v += *reinterpret_cast<const f32x4 *>(part + (size_t)q * NE16 * H + i);
     *reinterpret_cast<f32x4 *>(dw + i) = v;
 }
 
 struct BackWs {
-    size_t rows, cols, part_b, part, total;
-    int Tp, NEp, NE16, splits, per, nblk;
+    size_t rows, cols, part_b, on, part, total;
+    int Tp, NEp, NE16, splits, per, nblk, groups, eb;
 };
 static BackWs back_ws(const zeda_layer_desc *d)
 {
     const int NE = d->N + d->Z;
     const size_t es = d->dtype == ZEDA_BF16 ? 2 : 4;
     BackWs w;
-    w.nblk = ceil_div(d->T, kBackTokens);
-    w.Tp = w.nblk * kBackTokens;
+    w.Tp = ceil_div(d->T, 64) * 64;
+    w.nblk = w.Tp / kBackTokens;
     w.NEp = ceil_div(NE, 32) * 32;
     w.NE16 = ceil_div(NE, 16) * 16;
-    // token ranges: enough workgroups for the chip, whole blocks of 64 tokens
-    const int cols = ceil_div(d->H, 256) * ceil_div(w.NE16 / 16, 8);
-    int splits = ceil_div(512, cols);
-    if (splits > w.nblk) splits = w.nblk;
-    if (splits < 1) splits = 1;
-    w.per = ceil_div(w.nblk, splits) * kBackTokens;
-    w.splits = w.nblk ? ceil_div(w.Tp, w.per) : 0;
+    w.groups = ceil_div(w.NE16 / 16, kDwMaxBlocks);
+    w.eb = ceil_div(w.NE16 / 16, w.groups);
+    // token ranges, multiples of 128, so that some 512 workgroups share the product
+    int splits = ceil_div(512, ceil_div(d->H, 128) * w.groups);
+    const int most = ceil_div(w.Tp, 128);
+    if (splits > most) splits = most;
+    w.per = splits ? ceil_div(most, splits) * 128 : 128;
+    w.splits = ceil_div(w.Tp, w.per);
     size_t o = 0;
     auto take = [&](size_t bytes) { const size_t at = o; o += align_up(bytes ? bytes : 1, 256); return at; };
     const size_t n = (size_t)w.Tp * w.NEp * es;
     w.rows = take(n * (es == 2 ? 2 : 1));
     w.cols = take(n * (es == 2 ? 3 : 1));
     w.part_b = take((size_t)w.nblk * NE * 4);
+    w.on = take((size_t)w.nblk * 4);
     w.part = take((size_t)w.splits * w.NE16 * d->H * 4);
     w.total = o;
     return w;
@@ -514,7 +604,7 @@ static int launch_logit_grad(const LogitGrad &g, int nblk, hipStream_t s)
             return ZEDA_EHIP;
         done[dev] = true;
     }
-    logit_grad_kernel<F32><<<nblk, 256, kBackTokens * (g.NEp + 1) * 4, s>>>(g);
+    logit_grad_kernel<F32><<<nblk, kBackThreads, kBackTokens * (g.NEp + 1) * 4, s>>>(g);
     return last_launch_status();
 }
 
@@ -527,14 +617,15 @@ int launch_route_backward(const zeda_layer_desc *d, const void *x, const void *w
     const bool f32 = d->dtype != ZEDA_BF16;
     char *b = (char *)ws;
     float *part_b = (float *)(b + L.part_b), *part = (float *)(b + L.part);
+    uint32_t *on = (uint32_t *)(b + L.on);
     if (d->T > 0) {
         const LogitGrad g = {probs, gates, d_loss, d_gates, ids, counts, mask, d->T, d->N, NE, d->K, d->gate_norm, alpha, w,
-                             b + L.rows, b + L.cols, part_b, L.Tp, L.NEp};
+                             b + L.rows, b + L.cols, part_b, on, L.Tp, L.NEp};
         int rc = f32 ? launch_logit_grad<true>(g, L.nblk, s) : launch_logit_grad<false>(g, L.nblk, s);
         if (rc != ZEDA_OK) return rc;
         if (dx) {
             if (f32) {
-                router_dx_f32_kernel<<<dim3(L.nblk, ceil_div(H, 256)), 256, 0, s>>>((const float *)(b + L.rows), (const float *)wr, d->T, H, NE, L.NEp,
+                router_dx_f32_kernel<<<dim3(L.Tp / 64, ceil_div(H, 256)), 256, 0, s>>>((const float *)(b + L.rows), (const float *)wr, d->T, H, NE, L.NEp,
                                                                                    (float *)dx);
             } else {
                 const dim3 grid(ceil_div(d->T, kDxTokens), ceil_div(H, 256));
@@ -548,21 +639,21 @@ int launch_route_backward(const zeda_layer_desc *d, const void *x, const void *w
             if (hipGetLastError() != hipSuccess) return ZEDA_EHIP;
         }
         if (dw) {
-            const int blocks = L.NE16 / 16, groups = ceil_div(blocks, 8), eb = ceil_div(blocks, groups);
-            const dim3 grid(ceil_div(H, 256), L.splits, groups);
+            const dim3 grid(ceil_div(H, 128), L.splits, L.groups);
 #define ZEDA_DW(EB)                                                                                                                        \
-    if (f32) router_dw_kernel<EB, true><<<grid, 256, 0, s>>>(b + L.cols, x, mask, d->T, H, L.Tp, L.NEp, L.per, part, L.NE16);                  \
-    else router_dw_kernel<EB, false><<<grid, 256, 0, s>>>(b + L.cols, x, mask, d->T, H, L.Tp, L.NEp, L.per, part, L.NE16)
-            switch (eb) {
-                case 1: ZEDA_DW(1); break; case 2: ZEDA_DW(2); break; case 3: ZEDA_DW(3); break; case 4: ZEDA_DW(4); break;
-                case 5: ZEDA_DW(5); break; case 6: ZEDA_DW(6); break; case 7: ZEDA_DW(7); break; default: ZEDA_DW(8); break;
+    if (f32) router_dw_kernel<EB, true><<<grid, kDwThreads, 0, s>>>(b + L.cols, x, on, H, L.Tp, L.NEp, L.per, part, L.NE16);                  \
+    else router_dw_kernel<EB, false><<<grid, kDwThreads, 0, s>>>(b + L.cols, x, on, H, L.Tp, L.NEp, L.per, part, L.NE16)
+            switch (L.eb) {
+                case 1: ZEDA_DW(1); break; case 2: ZEDA_DW(2); break; case 3: ZEDA_DW(3); break;
+                case 4: ZEDA_DW(4); break; case 5: ZEDA_DW(5); break; default: ZEDA_DW(6); break;
             }
 #undef ZEDA_DW
             if (hipGetLastError() != hipSuccess) return ZEDA_EHIP;
         }
     }
     if (dw || dbias) {
-        reduce_dw_kernel<<<ceil_div(NE * H / 4, 256) + 1, 256, 0, s>>>(part, L.splits, NE, L.NE16, H, dw, part_b, L.nblk, dbias);
+        const int nw = dw ? ceil_div(NE * H / 4, 256) : 0, nb = dbias ? ceil_div(NE, kBiasExperts) : 0;
+        reduce_dw_kernel<<<nw + nb, 256, 0, s>>>(part, L.splits, NE, L.NE16, H, nw, dw, part_b, L.nblk, dbias);
         return last_launch_status();
     }
     return ZEDA_OK;
