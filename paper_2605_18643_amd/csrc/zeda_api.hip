@@ -131,9 +131,9 @@ static int forward_impl(const zeda_layer_desc *desc, const void *x, const void *
     const PlaceOut place = {offsets, sorted_slot, slot_to_row, num_real, num_real_out};
     // Few slots: the gate/up kernel places them, and selects for a handful of tokens (the tables it leaves are the same).
     TilePlace tp = {ids, place, gates, nullptr, router_bias, 0, 0, 0, desc->N + desc->Z, desc->gate_norm, false};
-    const bool places = !e8 && gateup_places(desc);
+    const bool places = e8 ? fp8_places(desc) : gateup_places(desc), selects = e8 ? fp8_selects(desc) : gateup_selects(desc);
     if (places) {
-        if ((rc = launch_route(desc, x, w_router, router_bias, ids, gates, route_ws, nullptr, nullptr, gateup_selects(desc) ? &tp : nullptr, s)) != ZEDA_OK) return rc;
+        if ((rc = launch_route(desc, x, w_router, router_bias, ids, gates, route_ws, nullptr, nullptr, selects ? &tp : nullptr, s)) != ZEDA_OK) return rc;
         mark(1 + ZEDA_STAGE_ROUTE);
     } else if (route_places(desc)) {
         if ((rc = launch_route(desc, x, w_router, router_bias, ids, gates, route_ws, nullptr, &place, nullptr, s)) != ZEDA_OK) return rc;
@@ -151,7 +151,7 @@ static int forward_impl(const zeda_layer_desc *desc, const void *x, const void *
     mark(1 + ZEDA_STAGE_DISPATCH);
     const int16_t *y_exp = nullptr;
     if (e8) {
-        if ((rc = launch_ffn_fp8(desc, x, e8, offsets, sorted_slot, y_slot, &y_exp, act, s)) != ZEDA_OK) return rc;
+        if ((rc = launch_ffn_fp8(desc, x, e8, offsets, sorted_slot, y_slot, &y_exp, act, places ? &tp : nullptr, s)) != ZEDA_OK) return rc;
     } else {
         if ((rc = launch_gateup(desc, x, w_gate, w_up, offsets, sorted_slot, act, places ? &tp : nullptr, s)) != ZEDA_OK) return rc;
         mark(1 + ZEDA_STAGE_GATEUP);
@@ -615,7 +615,7 @@ int zeda_expert_ffn_fp8(const zeda_layer_desc *desc, const void *x, const zeda_f
     if (ws_bytes < fp8_ffn_ws_bytes(desc)) return ZEDA_EWORKSPACE;
     if (desc->T == 0) return ZEDA_OK;
     // num_real equals expert_offsets[N], which the kernels read
-    return launch_ffn_fp8(desc, x, experts, expert_offsets, sorted_slot, y_slot, nullptr, ws, (hipStream_t)stream);
+    return launch_ffn_fp8(desc, x, experts, expert_offsets, sorted_slot, y_slot, nullptr, ws, nullptr, (hipStream_t)stream);
 }
 
 int zeda_moe_forward_fp8(const zeda_layer_desc *desc, const void *x, const void *w_router, const float *router_bias,

@@ -39,6 +39,13 @@ size_t fp8_ffn_ws_bytes(const zeda_layer_desc *d);
 // y_exp: NULL (y_slot receives bf16), or receives where the exponents of the rows' 128-column blocks are (y_slot: fp16, for
 // launch_combine_scaled)
 int launch_ffn_fp8(const zeda_layer_desc *d, const void *x, const zeda_fp8_experts *e, const int32_t *offsets, const int32_t *sorted_slot,
-                   void *y_slot, const int16_t **y_exp, void *ws, hipStream_t s);
+                   void *y_slot, const int16_t **y_exp, void *ws, const TilePlace *tp, hipStream_t s);
+// the same for small batches; act: fp32 scratch [T*K][I]
+int64_t fp8_few_slots(const zeda_layer_desc *d);  // T * K up to which these are the better ones; 0: never
+inline bool fp8_few(const zeda_layer_desc *d) { return (int64_t)d->T * d->K <= fp8_few_slots(d); }
+bool fp8_places(const zeda_layer_desc *d);   // its gate/up kernel places the slots (tp is given; offsets and sorted_slot are then outputs)
+bool fp8_selects(const zeda_layer_desc *d);  // ... and selects, from the partial logits of the router's first kernel
+int launch_ffn_fp8_few(const zeda_layer_desc *d, const void *x, const zeda_fp8_experts *e, const int32_t *offsets, const int32_t *sorted_slot,
+                       void *y_slot, int16_t *y_exp, float *act, int log_terms, const TilePlace *tp, hipStream_t s);
 
 }  // namespace zeda

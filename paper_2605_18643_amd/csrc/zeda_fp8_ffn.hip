@@ -301,7 +301,9 @@ static F8Ws fp8_ws(const zeda_layer_desc *d)
     auto take = [&](size_t bytes) { const size_t at = o; o += align_up(bytes ? bytes : 1, 256); return at; };
     w.x = take((size_t)d->T * d->H);
     w.xs = take((size_t)d->T * fp8_pitch(d->H));
-    w.act = take(S * fp8_cols(d->I));
+    // (fp32 for small batches; never less for a longer batch: callers size workspaces once, for their longest)
+    const size_t few = fp8_few_slots(d), most = S < few ? S : few;
+    w.act = take(S * fp8_cols(d->I) > most * 4 * d->I ? S * fp8_cols(d->I) : most * 4 * d->I);
     w.act_s = take(S * fp8_pitch(d->I));
     w.y_exp = take(S * (d->H / kFp8Block) * 2);
     w.total = o;
@@ -328,11 +330,16 @@ static int launch_f8(const F8Args &a, int S, hipStream_t s)
 }
 
 int launch_ffn_fp8(const zeda_layer_desc *d, const void *x, const zeda_fp8_experts *e, const int32_t *offsets, const int32_t *sorted_slot,
-                   void *y_slot, const int16_t **y_exp, void *ws, hipStream_t s)
+                   void *y_slot, const int16_t **y_exp, void *ws, const TilePlace *tp, hipStream_t s)
 {
     const F8Ws L = fp8_ws(d);
     uint8_t *w = (uint8_t *)ws;
     const int S = d->T * d->K, Ip = fp8_cols(d->I);
+    int log_terms = 18;
+    while ((1 << (log_terms - 18)) < Ip) ++log_terms;  // (448 * 448 < 2^18)
+    if (y_exp) *y_exp = (int16_t *)(w + L.y_exp);
+    if (fp8_few(d))
+        return launch_ffn_fp8_few(d, x, e, offsets, sorted_slot, y_slot, y_exp ? (int16_t *)(w + L.y_exp) : nullptr, (float *)(w + L.act), log_terms, tp, s);
     int rc = launch_quantize_rows(d->T, d->H, d->dtype, x, w + L.x, d->H, w + L.xs, fp8_pitch(d->H), s);
     if (rc != ZEDA_OK) return rc;
     F8Args a = {};
@@ -348,8 +355,8 @@ int launch_ffn_fp8(const zeda_layer_desc *d, const void *x, const zeda_fp8_exper
     a.y = y_slot;
     a.nft = ceil_div(d->H, 256);
     if (!y_exp) return launch_f8<kF8Down>(a, S, s);
-    *y_exp = a.y_exp = (int16_t *)(w + L.y_exp);
-    for (a.log_terms = 18; (1 << (a.log_terms - 18)) < Ip; ++a.log_terms) {}  // (448 * 448 < 2^18)
+    a.y_exp = (int16_t *)(w + L.y_exp);
+    a.log_terms = log_terms;
     return launch_f8<kF8DownScaled>(a, S, s);
 }
 
