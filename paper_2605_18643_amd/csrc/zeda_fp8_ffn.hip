@@ -2,6 +2,7 @@
 //   xq = Q(x), h = silu(G xq) .* (U xq), y = D Q(h),
 // Q = rounding to e4m3 under a power-of-two scale for every 128 columns, G, U, D e4m3 under one for every 128 x 128 block.
 #include <type_traits>
+#include <utility>
 
 #include "zeda_fp8.h"
 #include "zeda_lds.h"
@@ -67,7 +68,10 @@ enum { kF8GateUp = 0, kF8Down = 1, kF8DownScaled = 2 };
 constexpr int kF8Slot = kF8Tok * kFp8Block, kF8Ring = 3 * kF8Slot;
 
 // Gate/up: 128 activations (256 weight rows, eight units) a workgroup; down: 256 output columns.
-template <int KIND>
+template <typename F, int... S>
+__device__ __forceinline__ void for_steps(F &f, std::integer_sequence<int, S...>) { (f(std::integral_constant<int, S>{}), ...); }
+
+template <int KIND, int ODD>  // ODD: the number of chunks is odd
 struct F8Kernel {
     static constexpr bool GATEUP = KIND == kF8GateUp;
     const F8Args &a;
@@ -83,7 +87,15 @@ struct F8Kernel {
         const int rbs = GATEUP ? a.Ip / 16 : a.H / 32, rb = ft * 8 + wave * 2;
         const uint8_t *wp[2];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) wp[u] = a.w + ((size_t)e * rbs + min(rb + u, rbs - 1)) * (2 * nk) * kFp8Unit + lane * 16;
+        for (int u = 0; u < 2; ++u) wp[u] = a.w + ((size_t)e * rbs + min(rb + u, rbs - 1)) * (2 * nk) * kFp8Unit;
+        u32x4 wa[2][2][4];
+        auto load_w = [&](u32x4 (&d)[2][4], int c) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) d[u][q] = *reinterpret_cast<const u32x4 *>(wp[u] + (size_t)c * (2 * kFp8Unit) + q * 1024 + lane * 16);
+        };
+        load_w(wa[0], 0);  // (what an item starts from is asked for before anything waits: weights, token rows, scales)
         // This thread's piece of the token rows of every 32-row block: row tid / 8, and the ring's position tid % 8 of that row, where
         // the row's 16-byte pieces stand permuted by the row: 16 lanes that read one piece of 16 rows touch all banks once.
         const uint8_t *tp[NB];
@@ -92,22 +104,7 @@ struct F8Kernel {
             const int r = row0 + min(32 * b + (tid >> 3), rows - 1);
             tp[b] = a.src + (size_t)(GATEUP ? a.sorted_slot[r] / a.K : r) * ld + (((tid & 7) ^ ((tid >> 4) & 7)) << 4);
         }
-        // scales: one LDS row per token row, then one (two: gate, up) for the weights
-        for (int i = tid; i < NB * 32 * (pitch / 4); i += kF8Threads) {
-            const int r = i / (pitch / 4), c = i - r * (pitch / 4), rr = row0 + min(r, rows - 1);
-            reinterpret_cast<uint32_t *>(tab)[i] =
-                reinterpret_cast<const uint32_t *>(a.src_s + (size_t)(GATEUP ? a.sorted_slot[rr] / a.K : rr) * pitch)[c];
-        }
         uint8_t *wtab = tab + kF8Tok * pitch;
-        {
-            // (down: a workgroup's 256 rows are two blocks of 128)
-            const size_t r0 = GATEUP ? ((size_t)e * (a.Ip / kFp8Block) + ft) * 2 : (size_t)e * (a.H / kFp8Block) + ft * 2;
-            const int last = GATEUP ? 1 : min(1, a.H / kFp8Block - 1 - ft * 2);
-            for (int i = tid; i < 2 * (pitch / 4); i += kF8Threads) {
-                const int r = i / (pitch / 4), c = i - r * (pitch / 4);
-                reinterpret_cast<uint32_t *>(wtab)[i] = reinterpret_cast<const uint32_t *>(a.ws + (r0 + min(r, last)) * pitch)[c];
-            }
-        }
         const uint32_t my_ws = lds_addr(wtab + (GATEUP ? l32 >> 4 : wave >> 1) * pitch), my_ts = lds_addr(tab + l32 * pitch);
 
         f32x16 acc[2][NB];
@@ -121,13 +118,6 @@ struct F8Kernel {
         // Per chunk of 128 columns a wave fetches its weights into registers, one chunk ahead, and a quarter of the token rows
         // into the ring, two chunks ahead.  Loads return in order, so a wave that has used chunk c's weights has the token rows
         // of chunk c + 1 in the ring.
-        u32x4 wa[2][2][4];
-        auto load_w = [&](u32x4 (&d)[2][4], int c) {
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) d[u][q] = *reinterpret_cast<const u32x4 *>(wp[u] + (size_t)c * (2 * kFp8Unit) + q * 1024);
-        };
         auto load_t = [&](int c, int slot) {
 #pragma unroll
             for (int b = 0; b < NB; ++b)
@@ -146,46 +136,82 @@ struct F8Kernel {
                 for (int b = 0; b < NB; ++b) lds_wait(ts[b]);
             }
             const int sa = (int)(wsc >> (8 * (c & 3)));
-            const uint32_t at = ring0 + slot * kF8Slot + l32 * kFp8Block;
+            uint32_t at = ring0 + slot * kF8Slot + l32 * kFp8Block;
+            asm volatile("" : "+v"(at));  // (four addresses a chunk; those of all chunks would stay in registers)
+            const uint32_t at4[4] = {at + ((half ^ sw) << 4), at + (((2 + half) ^ sw) << 4), at + (((4 + half) ^ sw) << 4), at + (((6 + half) ^ sw) << 4)};
             u32x4 t[2][2];
-            auto fetch = [&](u32x4 (&d)[2], int s) {  // step s: half s % 2 of the chunk's columns of token block s / 2
-                d[0] = lds_read_b128(at + (s >> 1) * 4096 + (((4 * (s & 1) + half) ^ sw) << 4));
-                d[1] = lds_read_b128(at + (s >> 1) * 4096 + (((4 * (s & 1) + 2 + half) ^ sw) << 4));
+            // Step s: half s / NB of the chunk's columns of token block s % NB.  (The other way round, the two halves' products into the
+            // same accumulators would follow each other.)
+            auto fetch = [&](auto step) {
+                constexpr int s = decltype(step)::value, b = s % NB, m = s / NB;
+                t[s & 1][0] = lds_read_b128_at<b * 4096>(at4[2 * m]);
+                t[s & 1][1] = lds_read_b128_at<b * 4096>(at4[2 * m + 1]);
             };
-            fetch(t[0], 0);
-#pragma unroll
-            for (int s = 0; s < 2 * NB; ++s) {
-                if (s + 1 < 2 * NB) {
-                    fetch(t[(s + 1) & 1], s + 1);
+            fetch(std::integral_constant<int, 0>{});
+            auto step = [&](auto sc) {
+                constexpr int s = decltype(sc)::value, b = s % NB, m = s / NB;
+                if constexpr (s + 1 < 2 * NB) {
+                    fetch(std::integral_constant<int, s + 1>{});
                     lds_wait_but<2>(t[s & 1][0], t[s & 1][1]);
                 } else {
                     lds_wait(t[s & 1][0], t[s & 1][1]);
                 }
-                const int b = s >> 1, m = s & 1, sb = (int)(ts[b] >> (8 * (c & 3)));
                 const i32x8 tb = __builtin_bit_cast(i32x8, __builtin_shufflevector(t[s & 1][0], t[s & 1][1], 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
                     const i32x8 wu = __builtin_bit_cast(i32x8, __builtin_shufflevector(w[u][2 * m], w[u][2 * m + 1], 0, 1, 2, 3, 4, 5, 6, 7));
-                    acc[u][b] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wu, tb, acc[u][b], 0, 0, 0, sa, 0, sb);
+                    acc[u][b] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wu, tb, acc[u][b], 0, 0, 0, sa, 0, (int)(ts[b] >> (8 * (c & 3))));
                 }
-            }
+                asm volatile("" : "+v"(acc[0][b]), "+v"(acc[1][b]));  // (here and not after later reads, whose fragments would all stay in registers)
+            };
+            for_steps(step, std::make_integer_sequence<int, 2 * NB>{});
         };
         int slot = 0;
-        auto chunk = [&](const u32x4 (&w)[2][4], u32x4 (&next)[2][4], int c) {
-            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(NB + 8) : "memory");  // chunk c's token rows (behind them: chunk c + 1's, chunk c's weights)
-            asm volatile("s_barrier" ::: "memory");                        // everyone's; and everyone is done with chunk c - 1
-            load_t(min(c + 2, nk - 1), slot == 0 ? 2 : slot - 1);
-            load_w(next, min(c + 1, nk - 1));
-            multiply(w, c, slot);
+        // LEFT: chunks that follow this one, two at most; nothing is asked for past the last one
+        auto chunk = [&](const u32x4 (&w)[2][4], u32x4 (&next)[2][4], int c, auto left) {
+            constexpr int LEFT = decltype(left)::value;
+            // chunk c's token rows (behind them: chunk c's weights and chunk c + 1's rows)
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"((LEFT >= 1 ? NB : 0) + 8) : "memory");
+            asm volatile("s_barrier" ::: "memory");  // everyone's; and everyone is done with chunk c - 1
+            if constexpr (LEFT >= 2) load_t(min(c + 2, nk - 1), slot == 0 ? 2 : slot - 1);
+            if constexpr (LEFT >= 1) load_w(next, min(c + 1, nk - 1));
+            if (!ODD || c < nk) multiply(w, c, slot);  // (a single chunk: the two behind it are left out)
             slot = slot == 2 ? 0 : slot + 1;
         };
+        constexpr std::integral_constant<int, 0> none{};
+        constexpr std::integral_constant<int, 1> one{};
+        constexpr std::integral_constant<int, 2> two{};
         load_t(0, 0);
         load_t(min(1, nk - 1), 1);
-        load_w(wa[0], 0);
+        // scales: one LDS row per token row, then one (two: gate, up) for the weights
+        for (int i = tid; i < NB * 32 * (pitch / 4); i += kF8Threads) {
+            const int r = i / (pitch / 4), c = i - r * (pitch / 4), rr = row0 + min(r, rows - 1);
+            reinterpret_cast<uint32_t *>(tab)[i] =
+                reinterpret_cast<const uint32_t *>(a.src_s + (size_t)(GATEUP ? a.sorted_slot[rr] / a.K : rr) * pitch)[c];
+        }
+        {
+            // (down: a workgroup's 256 rows are two blocks of 128)
+            const size_t r0 = GATEUP ? ((size_t)e * (a.Ip / kFp8Block) + ft) * 2 : (size_t)e * (a.H / kFp8Block) + ft * 2;
+            const int last = GATEUP ? 1 : min(1, a.H / kFp8Block - 1 - ft * 2);
+            for (int i = tid; i < 2 * (pitch / 4); i += kF8Threads) {
+                const int r = i / (pitch / 4), c = i - r * (pitch / 4);
+                reinterpret_cast<uint32_t *>(wtab)[i] = reinterpret_cast<const uint32_t *>(a.ws + (r0 + min(r, last)) * pitch)[c];
+            }
+        }
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the scale tables are written (met by the first barrier)
-        for (int c = 0; c < nk; c += 2) {
-            chunk(wa[0], wa[1], c);
-            if (c + 1 < nk) chunk(wa[1], wa[0], c + 1);
+        int c = 0;
+        for (; c + 2 + ODD < nk; c += 2) {
+            chunk(wa[0], wa[1], c, two);
+            chunk(wa[1], wa[0], c + 1, two);
+        }
+        // (straight on: paths that meet again would hold all accumulators twice)
+        if constexpr (ODD) {
+            chunk(wa[0], wa[1], c, two);
+            chunk(wa[1], wa[0], c + 1, one);
+            chunk(wa[0], wa[1], c + 2, none);
+        } else {
+            chunk(wa[0], wa[1], c, one);
+            chunk(wa[1], wa[0], c + 1, none);
         }
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();  // everyone is done with the ring
@@ -201,7 +227,7 @@ struct F8Kernel {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         const float g = acc[u][b][i];
-                        h[u][b][i] = g / (1.0f + __expf(-g)) * acc[u][b][i + 8];
+                        h[u][b][i] = g * __builtin_amdgcn_rcpf(1.0f + __expf(-g)) * acc[u][b][i + 8];
                         mx[b] = fmaxf(mx[b], finite_abs(h[u][b][i]));
                     }
                 mx[b] = fmaxf(mx[b], __shfl_xor(mx[b], 32));
@@ -269,7 +295,7 @@ struct F8Kernel {
     }
 };
 
-template <int KIND>
+template <int KIND, int ODD>
 __global__ __launch_bounds__(kF8Threads, 2) void ffn_fp8_kernel(F8Args a)
 {
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
@@ -281,7 +307,7 @@ __global__ __launch_bounds__(kF8Threads, 2) void ffn_fp8_kernel(F8Args a)
     if (idx >= per || item >= items) return;
     const int tile = item / a.nft, ft = item - tile * a.nft;
     const int3 at = t.locate(tile);
-    const F8Kernel<KIND> k = {a, lds, lds + kF8Ring, at.x, at.y, at.z, ft};
+    const F8Kernel<KIND, ODD> k = {a, lds, lds + kF8Ring, at.x, at.y, at.z, ft};
     const int nb = (at.z + 31) >> 5;
     if (nb == 1) k.template run<1>();
     else if (nb == 2) k.template run<2>();
@@ -311,8 +337,8 @@ static F8Ws fp8_ws(const zeda_layer_desc *d)
 }
 size_t fp8_ffn_ws_bytes(const zeda_layer_desc *d) { return fp8_ws(d).total; }
 
-template <int KIND>
-static int launch_f8(const F8Args &a, int S, hipStream_t s)
+template <int KIND, int ODD>
+static int launch_f8_chunks(const F8Args &a, int S, hipStream_t s)
 {
     const int pitch = fp8_pitch(KIND == kF8GateUp ? a.H : a.Ip), tab = (kF8Tok + 2) * pitch, bytes = kF8Ring + (tab > 4 * kF8Tok * 4 ? tab : 4 * kF8Tok * 4);
     static bool done[kMaxDevices] = {};  // per instantiation and device (idempotent)
@@ -320,13 +346,19 @@ static int launch_f8(const F8Args &a, int S, hipStream_t s)
     if (dev < 0) return ZEDA_EHIP;
     if (!done[dev]) {
         constexpr int most = kF8Ring + (kF8Tok + 2) * (kFp8MaxWidth / kFp8Block);
-        if (hipFuncSetAttribute((const void *)ffn_fp8_kernel<KIND>, hipFuncAttributeMaxDynamicSharedMemorySize, most) != hipSuccess) return ZEDA_EHIP;
+        if (hipFuncSetAttribute((const void *)ffn_fp8_kernel<KIND, ODD>, hipFuncAttributeMaxDynamicSharedMemorySize, most) != hipSuccess) return ZEDA_EHIP;
         done[dev] = true;
     }
     const int64_t items = ((int64_t)S / kF8Tok + (a.N < S ? a.N : S)) * a.nft, grid = (items + 7) / 8 * 8;
     if (grid > 0x7fffffff) return ZEDA_EUNSUPPORTED;
-    ffn_fp8_kernel<KIND><<<(unsigned)grid, kF8Threads, bytes, s>>>(a);
+    ffn_fp8_kernel<KIND, ODD><<<(unsigned)grid, kF8Threads, bytes, s>>>(a);
     return last_launch_status();
+}
+
+template <int KIND>
+static int launch_f8(const F8Args &a, int S, hipStream_t s)
+{
+    return (KIND == kF8GateUp ? a.H : a.Ip) / kFp8Block % 2 ? launch_f8_chunks<KIND, 1>(a, S, s) : launch_f8_chunks<KIND, 0>(a, S, s);
 }
 
 int launch_ffn_fp8(const zeda_layer_desc *d, const void *x, const zeda_fp8_experts *e, const int32_t *offsets, const int32_t *sorted_slot,
