@@ -57,11 +57,21 @@ int launch_dispatch_counts(const zeda_layer_desc *d, const int32_t *ids, const u
 // Only the logits, without biases: `slices` tables [Tpad][E] over slices of the hidden dimension, added in order (a training step
 // selects from them and keeps the probabilities).
 struct RouteTables {
-    int slices, Tpad, E;
+    int slices, Tpad, E, tokens;  // tokens: of a workgroup
     size_t bytes() const { return (size_t)slices * Tpad * E * sizeof(float); }
 };
 RouteTables route_tables(const zeda_layer_desc *d);
 int launch_route_tables(const zeda_layer_desc *d, const void *x, const void *wr, float *tables, hipStream_t s);
+// What a training step's selection leaves beside ids and gates: probs[T][NE]; per workgroup the sums of the probabilities of the tokens that
+// count (mask, may be NULL), part_p[NE], and part_c[NE + 1], their slots on every expert and their number; *done = 0.
+struct TrainOut {
+    const uint8_t *mask;
+    float *probs, *part_p;
+    int32_t *part_c, *done;
+};
+// router and selection in one kernel: in bf16 where one kernel covers the hidden dimension
+bool route_train_fused(const zeda_layer_desc *d);
+int launch_route_train_fused(const zeda_layer_desc *d, const void *x, const void *wr, const float *bias, int32_t *ids, float *gates, const TrainOut &to, hipStream_t s);
 // Section 2.2 statistics over the batch of all T tokens (f, P: [N+Z]; summary: 7 floats); ws of routing_stats_ws_bytes
 int launch_routing_stats(const zeda_layer_desc *d, const void *x, const void *wr, const float *bias, float alpha, float w,
                          float *f, float *P, float *summary, void *ws, hipStream_t s);

@@ -107,7 +107,7 @@ struct RouteCfg {
     static constexpr int STAGES = MAX_LDS / STAGE < 8 ? MAX_LDS / STAGE : 8;
     static constexpr int LD = NB * 32 + 1;
     static constexpr int TABLES = KS * TOK * LD * 4;  // bytes of the logit tables, which reuse the ring, as do the counters
-    static constexpr int CNT_OFF = (TABLES + 15) / 16 * 16, END = CNT_OFF + TB * kMaxExperts * 4;
+    static constexpr int CNT_OFF = (TABLES + 15) / 16 * 16, END = CNT_OFF + (TB > 1 ? TB : 2) * kMaxExperts * 4;  // (TRAIN: two)
     static constexpr int LDS_BYTES = STAGES * STAGE > END ? STAGES * STAGE : END;
     static_assert(ROWS % RPI == 0 && STAGES >= 2 && LDS_BYTES <= MAX_LDS && GROUPS >= 1, "");
     static_assert((STAGES - 1) * ((NI + W - 1) / W) <= 63, "vmcnt is a 6-bit counter");
@@ -122,13 +122,14 @@ __device__ __forceinline__ void route_wait_vmcnt()
 
 // partial (may be NULL): receives the logits of the workgroup's slice of the hidden dimension instead of a selection.
 // cnt8, p_part (either may be NULL): see publish_blocks.
-template <int NB, int TB, int W>
+// TRAIN: a training step's outputs (see TrainOut) in place of cnt8 and p_part; no split.
+template <int NB, int TB, int W, bool TRAIN>
 __global__ __launch_bounds__(64 * W) void route_bf16_kernel(const bf16_t *__restrict__ x, const bf16_t *__restrict__ wr,
                                                                    const float *__restrict__ bias, int T, int H, int N, int NE,
                                                                    int K, int gate_norm, int32_t *__restrict__ ids,
                                                                    float *__restrict__ gates, float *__restrict__ partial, int Tpad,
                                                                    uint8_t *__restrict__ cnt8, int cnt_ld,
-                                                                   float *__restrict__ p_part)
+                                                                   float *__restrict__ p_part, TrainOut train)
 {
     typedef RouteCfg<NB, TB, W> C;
     extern __shared__ __attribute__((aligned(1024))) unsigned char lds[];
@@ -239,6 +240,35 @@ __global__ __launch_bounds__(64 * W) void route_bf16_kernel(const bf16_t *__rest
                 for (int q = 1; q < C::KS; ++q) v[k] += p[q * C::TOK * C::LD + k];
             }
             dst[i] = v;
+        }
+        return;
+    }
+    if constexpr (TRAIN) {
+        // counters of the whole workgroup, then which of its tokens count
+        static_assert(C::TOK <= kMaxExperts, "");
+        int *s_on = s_cnt + kMaxExperts;
+        for (int i = tid; i < kMaxExperts; i += C::THREADS) s_cnt[i] = 0;
+        const int nt = min(C::TOK, T - t0);
+        for (int i = tid; i < C::TOK; i += C::THREADS) s_on[i] = i < nt && (!train.mask || train.mask[t0 + i]);
+        __syncthreads();
+        for (int tk0 = 4 * wave; tk0 < C::TOK; tk0 += 4 * W) {
+            const int id = select_rows<2 * NB, C::KS>(lg, C::LD, C::TOK * C::LD, bias_c, tk0, C::TOK, t0, T, NE, N, K, gate_norm, ids, gates, lg, C::LD);
+            if ((unsigned)id < (unsigned)kMaxExperts && s_on[tk0 + (lane >> 4)]) atomicAdd(&s_cnt[id], 1);
+        }
+        __syncthreads();
+        for (int i = tid; i < nt * NE; i += C::THREADS) train.probs[(size_t)t0 * NE + i] = lg[(i / NE) * C::LD + i % NE];
+        for (int e = tid; e < NE; e += C::THREADS) {
+            float p = 0.f;
+#pragma unroll 16
+            for (int k = 0; k < C::TOK; ++k) p += s_on[k] ? lg[k * C::LD + e] : 0.f;
+            train.part_p[(size_t)blockIdx.x * NE + e] = p;
+            train.part_c[(size_t)blockIdx.x * (NE + 1) + e] = s_cnt[e];
+        }
+        if (tid == 0) {
+            int n = 0;
+            for (int k = 0; k < C::TOK; ++k) n += s_on[k];
+            train.part_c[(size_t)blockIdx.x * (NE + 1) + NE] = n;
+            if (blockIdx.x == 0) *train.done = 0;
         }
         return;
     }
@@ -430,6 +460,7 @@ struct RouteExtras {
     PlaceOut place;
     TilePlace *tp;  // given: the gate/up kernel selects
     bool tables;    // only the logit tables, for a selection of the caller's
+    const TrainOut *train;
 };
 
 template <int NB, int TB, int W>
@@ -437,19 +468,25 @@ static int launch_route_bf16(const zeda_layer_desc *d, const void *x, const void
                              float *gates, float *partial, int slices, const RouteExtras &ex, hipStream_t s)
 {
     typedef RouteCfg<NB, TB, W> C;
-    // the kernel uses more LDS than a launch gets by default: opt in once per kernel and device
+    // the kernels use more LDS than a launch gets by default: opt in once per kernel and device
     static bool done[kMaxDevices] = {};  // idempotent, so a race between host threads is harmless
     const int dev = current_device();
     if (dev < 0) return ZEDA_EHIP;
     if (!done[dev]) {
-        if (hipFuncSetAttribute((const void *)route_bf16_kernel<NB, TB, W>, hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS_BYTES) != hipSuccess)
+        if (hipFuncSetAttribute((const void *)route_bf16_kernel<NB, TB, W, false>, hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS_BYTES) != hipSuccess ||
+            hipFuncSetAttribute((const void *)route_bf16_kernel<NB, TB, W, true>, hipFuncAttributeMaxDynamicSharedMemorySize, C::LDS_BYTES) != hipSuccess)
             return ZEDA_EHIP;
         done[dev] = true;
     }
     const int NE = d->N + d->Z, Tpad = route_tpad(d);
-    route_bf16_kernel<NB, TB, W><<<dim3(ceil_div(d->T, C::TOK), slices), C::THREADS, C::LDS_BYTES, s>>>(
+    if (ex.train) {
+        route_bf16_kernel<NB, TB, W, true><<<ceil_div(d->T, C::TOK), C::THREADS, C::LDS_BYTES, s>>>(
+            (const bf16_t *)x, (const bf16_t *)wr, bias, d->T, d->H, d->N, NE, d->K, d->gate_norm, ids, gates, nullptr, Tpad, nullptr, 0, nullptr, *ex.train);
+        return last_launch_status();
+    }
+    route_bf16_kernel<NB, TB, W, false><<<dim3(ceil_div(d->T, C::TOK), slices), C::THREADS, C::LDS_BYTES, s>>>(
         (const bf16_t *)x, (const bf16_t *)wr, bias, d->T, d->H, d->N, NE, d->K, d->gate_norm, ids, gates, slices > 1 || ex.tables ? partial : nullptr, Tpad,
-        ex.cnt8, ex.cnt_ld, ex.p_part);
+        ex.cnt8, ex.cnt_ld, ex.p_part, TrainOut{});
     if (ex.tp && slices > 1) {
         ex.tp->partial = partial;
         ex.tp->slices = slices;
@@ -783,7 +820,7 @@ int launch_routing_stats(const zeda_layer_desc *d, const void *x, const void *wr
         float *partial = route_ws_bytes(d) ? (float *)ws : nullptr;
         uint8_t *cnt8 = (uint8_t *)ws + align_up(route_ws_bytes(d), 256);
         float *p_part = (float *)(cnt8 + route_counts_bytes(d));
-        const RouteExtras ex = {cnt8, route_counts_ld(d), p_part, {}, nullptr, false};
+        const RouteExtras ex = {cnt8, route_counts_ld(d), p_part, {}, nullptr, false, nullptr};
         const RoutePlan plan = route_plan(d, partial != nullptr);
         const int prows = ceil_div(d->T, plan.slices > 1 ? kSelectTokens : 16 * plan.tb);  // workgroups that select
         const int rc = launch_route_bf16_any(d, x, wr, bias, nullptr, nullptr, partial, ex, s);
@@ -819,12 +856,22 @@ int launch_routing_stats(const zeda_layer_desc *d, const void *x, const void *wr
 RouteTables route_tables(const zeda_layer_desc *d)
 {
     const int E = ceil_div(d->N + d->Z, 32) * 32;
-    return {d->dtype == ZEDA_BF16 ? route_plan(d, true).slices : 1, route_tpad(d), E};
+    if (d->dtype != ZEDA_BF16) return {1, route_tpad(d), E, kRouteF32Tokens};
+    const RoutePlan p = route_plan(d, true);
+    return {p.slices, route_tpad(d), E, 16 * p.tb};
+}
+bool route_train_fused(const zeda_layer_desc *d) { return d->dtype == ZEDA_BF16 && route_plan(d, true).slices == 1; }
+int launch_route_train_fused(const zeda_layer_desc *d, const void *x, const void *wr, const float *bias, int32_t *ids, float *gates, const TrainOut &to,
+                             hipStream_t s)
+{
+    // (without scratch the plan is the same one: the best of those without a split)
+    const RouteExtras ex = {nullptr, 0, nullptr, {}, nullptr, false, &to};
+    return launch_route_bf16_any(d, x, wr, bias, ids, gates, nullptr, ex, s);
 }
 int launch_route_tables(const zeda_layer_desc *d, const void *x, const void *wr, float *tables, hipStream_t s)
 {
     if (d->dtype != ZEDA_BF16) return launch_route_f32(d, x, wr, nullptr, nullptr, nullptr, tables, route_tables(d).E, s);
-    const RouteExtras ex = {nullptr, 0, nullptr, {}, nullptr, true};
+    const RouteExtras ex = {nullptr, 0, nullptr, {}, nullptr, true, nullptr};
     return launch_route_bf16_any(d, x, wr, nullptr, nullptr, nullptr, tables, ex, s);
 }
 
@@ -832,7 +879,7 @@ int launch_route(const zeda_layer_desc *d, const void *x, const void *wr, const 
                  float *partial, uint8_t *cnt8, const PlaceOut *place, TilePlace *tp, hipStream_t s)
 {
     if (d->dtype == ZEDA_BF16) {
-        const RouteExtras ex = {cnt8, cnt8 ? route_counts_ld(d) : 0, nullptr, place ? *place : PlaceOut{}, tp, false};
+        const RouteExtras ex = {cnt8, cnt8 ? route_counts_ld(d) : 0, nullptr, place ? *place : PlaceOut{}, tp, false, nullptr};
         return launch_route_bf16_any(d, x, wr, bias, ids, gates, partial, ex, s);
     }
     return launch_route_f32(d, x, wr, bias, ids, gates, nullptr, 0, s);

@@ -151,7 +151,7 @@ static TrainWs train_ws(const zeda_layer_desc *d)
     TrainWs w;
     size_t o = 0;
     auto take = [&](size_t bytes) { const size_t at = o; o += align_up(bytes ? bytes : 1, 256); return at; };
-    w.tables = take(route_tables(d).bytes());
+    w.tables = take(route_train_fused(d) ? 0 : route_tables(d).bytes());
     w.part_p = take(nblk * NE * 4);
     w.part_c = take(nblk * (NE + 1) * 4);
     w.done = take(4);
@@ -168,20 +168,25 @@ int launch_route_train(const zeda_layer_desc *d, const void *x, const void *wr, 
     float *tables = (float *)((char *)ws + L.tables), *part_p = (float *)((char *)ws + L.part_p);
     int32_t *part_c = (int32_t *)((char *)ws + L.part_c), *done = (int32_t *)((char *)ws + L.done);
     const int NE = d->N + d->Z, nblk = ceil_div(d->T, kTrainTokens);
+    const TrainOut to = {mask, probs, part_p, part_c, done};
     if (d->T == 0) {
         train_nothing_kernel<<<1, 256, 0, s>>>(NE, counts, P, summary);
         return last_launch_status();
     }
-    const int rc = launch_route_tables(d, x, wr, tables, s);
+    const bool fused = route_train_fused(d);
+    const int rows = fused ? ceil_div(d->T, t.tokens) : nblk;  // workgroups that select
+    const int rc = fused ? launch_route_train_fused(d, x, wr, bias, ids, gates, to, s) : launch_route_tables(d, x, wr, tables, s);
     if (rc != ZEDA_OK) return rc;
+    if (!fused) {
 #define ZEDA_TRAIN(NB) train_select_kernel<NB><<<nblk, 256, 0, s>>>(tables, t.slices, t.Tpad, bias, mask, d->T, d->N, NE, d->K, d->gate_norm, ids, gates, probs, part_p, part_c, done)
-    switch (t.E / 32) {
-        case 1: ZEDA_TRAIN(1); break; case 2: ZEDA_TRAIN(2); break; case 3: ZEDA_TRAIN(3); break; case 4: ZEDA_TRAIN(4); break;
-        case 5: ZEDA_TRAIN(5); break; case 6: ZEDA_TRAIN(6); break; case 7: ZEDA_TRAIN(7); break; default: ZEDA_TRAIN(8); break;
-    }
+        switch (t.E / 32) {
+            case 1: ZEDA_TRAIN(1); break; case 2: ZEDA_TRAIN(2); break; case 3: ZEDA_TRAIN(3); break; case 4: ZEDA_TRAIN(4); break;
+            case 5: ZEDA_TRAIN(5); break; case 6: ZEDA_TRAIN(6); break; case 7: ZEDA_TRAIN(7); break; default: ZEDA_TRAIN(8); break;
+        }
 #undef ZEDA_TRAIN
-    if (hipGetLastError() != hipSuccess) return ZEDA_EHIP;
-    train_final_kernel<<<ceil_div(NE, kFinalExperts), kFinalThreads, 0, s>>>(part_p, part_c, nblk, d->N, NE, d->K, alpha, w, counts, P, summary, done);
+        if (hipGetLastError() != hipSuccess) return ZEDA_EHIP;
+    }
+    train_final_kernel<<<ceil_div(NE, kFinalExperts), kFinalThreads, 0, s>>>(part_p, part_c, rows, d->N, NE, d->K, alpha, w, counts, P, summary, done);
     return last_launch_status();
 }
 
@@ -261,41 +266,49 @@ __global__ __launch_bounds__(kBackThreads) void logit_grad_kernel(LogitGrad a)
             s_a[lane + 64 * q] = (float)(kA / NE * ((double)c[q] * NE - (cE + cZ)) + (lane + 64 * q < N ? apart * (NE - N) : -apart * N));
     }
     __syncthreads();
+    // (the tokens side by side: each step is a broadcast from one lane and four comparisons)
+    float u[PER][4], g_of[PER][4] = {}, v_of[PER][4] = {}, sum[PER] = {};
 #pragma unroll
-    for (int k = 0; k < PER; ++k) {
-        float dl[4] = {0.f, 0.f, 0.f, 0.f};
-        if (on[k]) {
-            float u[4], g_of[4] = {}, v_of[4] = {}, s = 0.f, pa = 0.f;
+    for (int q = 0; q < 4; ++q) {
+        const float slope = lane + 64 * q < NE ? s_a[lane + 64 * q] : 0.f;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) u[q] = lane + 64 * q < NE ? s_a[lane + 64 * q] : 0.f;
-            if (a.d_gates) {
-                for (int j = 0; j < a.K; ++j) {
-                    const int ej = __builtin_amdgcn_readlane(id[k], j);
-                    const float gj = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(g[k]), j));
-                    const float dj = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(dg[k]), j));
-                    s = fmaf(gj, dj, s);
+        for (int k = 0; k < PER; ++k) u[k][q] = slope;
+    }
+    if (a.d_gates) {
+        const bool softmax = a.gate_norm == ZEDA_GATE_SOFTMAX;
+        const int within = a.gate_norm == ZEDA_GATE_TOPK_NORM ? NE : N;
+        for (int j = 0; j < a.K; ++j) {
 #pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        if (ej == lane + 64 * q) {
-                            if (a.gate_norm == ZEDA_GATE_SOFTMAX) {
-                                u[q] += dj;
-                            } else {
-                                v_of[q] = fmaf(gj, dj, v_of[q]);
-                                if (a.gate_norm == ZEDA_GATE_TOPK_NORM || ej < N) g_of[q] += gj;
-                            }
-                        }
+            for (int k = 0; k < PER; ++k) {
+                const int ej = __builtin_amdgcn_readlane(id[k], j);
+                const float gj = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(g[k]), j));
+                const float dj = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(dg[k]), j));
+                const float direct = softmax ? dj : 0.f, shared = softmax ? 0.f : gj, in = ej < within ? shared : 0.f;
+                sum[k] = fmaf(gj, dj, sum[k]);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const bool mine = ej == lane + 64 * q;
+                    u[k][q] += mine ? direct : 0.f;
+                    v_of[k][q] += mine ? shared * dj : 0.f;
+                    g_of[k][q] += mine ? in : 0.f;
                 }
             }
-#pragma unroll
-            for (int q = 0; q < 4; ++q) pa = fmaf(p[k][q], u[q], pa);
-            pa = wave_sum(pa);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) dl[q] = lane + 64 * q < NE ? p[k][q] * (u[q] - pa) + (v_of[q] - s * g_of[q]) : 0.f;
         }
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-            if (lane + 64 * q < a.NEp) s_dl[(wave * PER + k) * LD + lane + 64 * q] = dl[q];
     }
+    float pa[PER] = {};
+#pragma unroll
+    for (int k = 0; k < PER; ++k) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) pa[k] = fmaf(p[k][q], u[k][q], pa[k]);
+        pa[k] = wave_sum(pa[k]);
+    }
+#pragma unroll
+    for (int k = 0; k < PER; ++k)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const float dl = on[k] && lane + 64 * q < NE ? p[k][q] * (u[k][q] - pa[k]) + (v_of[k][q] - (g_of[k][q] != 0.f ? sum[k] * g_of[k][q] : 0.f)) : 0.f;
+            if (lane + 64 * q < a.NEp) s_dl[(wave * PER + k) * LD + lane + 64 * q] = dl;
+        }
     __syncthreads();
     if (tid < NE) {
         double b = 0.;
@@ -574,8 +587,8 @@ static BackWs back_ws(const zeda_layer_desc *d)
     w.NE16 = ceil_div(NE, 16) * 16;
     w.groups = ceil_div(w.NE16 / 16, kDwMaxBlocks);
     w.eb = ceil_div(w.NE16 / 16, w.groups);
-    // token ranges, multiples of 128, so that some 512 workgroups share the product
-    int splits = ceil_div(512, ceil_div(d->H, 128) * w.groups);
+    // token ranges, multiples of 128, so that some 256 workgroups share the product
+    int splits = ceil_div(256, ceil_div(d->H, 128) * w.groups);
     const int most = ceil_div(w.Tp, 128);
     if (splits > most) splits = most;
     w.per = splits ? ceil_div(most, splits) * 128 : 128;

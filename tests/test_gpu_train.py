@@ -68,7 +68,8 @@ def _batch_sums(p, ids, on, N, K):
 
 SHAPES = [(1, 128, 8, 4, 2, "bf16"), (15, 256, 3, 0, 3, "bf16"), (16, 128, 20, 12, 6, "bf16"), (17, 384, 24, 8, 3, "bf16"), (64, 2048, 128, 32, 8, "bf16"),
           (65, 128, 1, 0, 1, "bf16"), (333, 512, 64, 32, 4, "bf16"), (1500, 256, 128, 64, 8, "bf16"), (130, 128, 250, 6, 16, "bf16"),
-          (2, 64, 8, 4, 2, "f32"), (77, 260, 33, 7, 5, "f32"), (513, 1024, 32, 8, 4, "f32"), (40, 36, 200, 56, 16, "f32"), (5000, 128, 16, 8, 2, "bf16")]
+          (2, 64, 8, 4, 2, "f32"), (77, 260, 33, 7, 5, "f32"), (513, 1024, 32, 8, 4, "f32"), (40, 36, 200, 56, 16, "f32"), (5000, 128, 16, 8, 2, "bf16"),
+          (8201, 128, 60, 4, 4, "bf16"), (8500, 128, 224, 32, 8, "bf16"), (4099, 256, 100, 28, 8, "bf16")]
 
 
 @pytest.mark.parametrize("T, H, N, Z, K, dtype", SHAPES)
