@@ -170,7 +170,7 @@ struct F8Kernel {
         // LEFT: chunks that follow this one, two at most; nothing is asked for past the last one
         auto chunk = [&](const u32x4 (&w)[2][4], u32x4 (&next)[2][4], int c, auto left) {
             constexpr int LEFT = decltype(left)::value;
-            // chunk c's token rows (behind them: chunk c's weights and chunk c + 1's rows)
+            // chunk c's token rows (behind them: chunk c's weights and chunk c + 1's rows; of the first chunk see below)
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"((LEFT >= 1 ? NB : 0) + 8) : "memory");
             asm volatile("s_barrier" ::: "memory");  // everyone's; and everyone is done with chunk c - 1
             if constexpr (LEFT >= 2) load_t(min(c + 2, nk - 1), slot == 0 ? 2 : slot - 1);
@@ -198,7 +198,10 @@ struct F8Kernel {
                 reinterpret_cast<uint32_t *>(wtab)[i] = reinterpret_cast<const uint32_t *>(a.ws + (r0 + min(r, last)) * pitch)[c];
             }
         }
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the scale tables are written (met by the first barrier)
+        // The first chunk's weights were asked for before its token rows, so the count that a chunk waits for does not cover these: all but the
+        // second chunk's rows are awaited here (a wave that fetches no scales has nothing else that waits).  And the scale tables are
+        // written.  Both are met by the first barrier.
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(NB) : "memory");
         int c = 0;
         for (; c + 2 + ODD < nk; c += 2) {
             chunk(wa[0], wa[1], c, two);

@@ -307,6 +307,32 @@ def test_the_same_bits_again_on_another_stream_and_in_a_graph():
         (x.float() @ x.float().t()).sum().item()
 
 
+@pytest.mark.parametrize("H, I", [(512, 256), (640, 384), (1024, 704), (2048, 768)])
+def test_tiles_of_all_sizes_keep_their_bits_after_other_data(H, I):
+    """Rows of one to four 32-row blocks per tile, and between the runs the same kernels on data whose every value is a NaN: what a workgroup
+    finds in its shared memory must not reach the result."""
+    loads = [1, 20, 40, 64, 70, 96, 100, 128, 5, 33, 129, 160] * 4
+    N, T = len(loads), sum(loads)
+    w, d = _layer(T, H, I, N, 1, 1)
+    qs = [zeda.zeda_quantize_weights_fp8(m.contiguous()) for m in synth.draw_experts(w, "cuda")]
+    packed, x = zeda.zeda_pack_expert_weights_fp8(d, *[t for p in qs for t in p]), synth.draw_tokens(w, "cuda")
+    ids = torch.tensor(np.repeat(np.arange(N), loads), dtype=torch.int32, device="cuda").view(T, 1)
+    off, ss, _, nr = _dispatch(d, ids)
+    bad = torch.full_like(x, float("nan"))
+    ws = torch.empty(zeda.expert_ffn_workspace_bytes_fp8(d), dtype=torch.uint8, device="cuda")
+
+    def run(rows):
+        y = torch.zeros(T, H, dtype=torch.bfloat16, device="cuda")
+        zeda.zeda_expert_ffn_fp8(d, rows, packed, off, ss, nr, y, ws)
+        return y
+
+    first = run(x)
+    assert torch.isfinite(first).all()
+    for rep in range(12):
+        assert torch.isnan(run(bad)).all()
+        assert torch.equal(run(x), first), rep
+
+
 @pytest.mark.parametrize("T", [1, 24, 333])
 def test_residual_block_and_stack(T):
     w, d = _layer(T, 256, 192, 6, 3, 3)
