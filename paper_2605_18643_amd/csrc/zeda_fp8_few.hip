@@ -13,7 +13,7 @@
 namespace zeda {
 
 constexpr int kF8FewThreads = 256, kF8FewWaves = 4, kF8FewRows = 16;
-constexpr int kF8FewDepth = 8;  // units of a wave in flight: 16 KiB
+constexpr int kF8FewDepth = 4;  // units in flight of a wave and row block (gate/up: eight leave room for three waves a SIMD, 126.1 us for the layer of 64 tokens; four 115.0)
 
 template <typename T> __device__ __forceinline__ void few_load8(const T *p, float (&v)[8]);
 template <> __device__ __forceinline__ void few_load8<bf16_t>(const bf16_t *p, float (&v)[8])
@@ -31,7 +31,8 @@ template <> __device__ __forceinline__ void few_load8<float>(const float *p, flo
 
 // LDS: a row's columns at row * (cols + 16) (16 rows' pieces then start in different banks), its scales behind all rows
 __host__ __device__ constexpr int few_row(int cols) { return cols + 16; }
-__host__ __device__ constexpr int few_rows_bytes(int cols) { return kF8FewRows * (few_row(cols) + cols / kFp8Block); }
+// (and behind them gate/up's weight scales)
+__host__ __device__ constexpr int few_rows_bytes(int cols) { return kF8FewRows * (few_row(cols) + cols / kFp8Block) + 2 * (cols / kFp8Block); }
 // ... and when the rows have been multiplied, the waves' sums of nf unit row blocks
 __host__ __device__ constexpr int few_lds(int cols, int nf)
 {
@@ -61,11 +62,25 @@ __device__ __forceinline__ void few_quantize(uint8_t *lds, int rows, int src_col
     }
 }
 
+// eight e4m3 values (two words) as bf16, exactly
+__device__ __forceinline__ bf16x8 few_widen(uint32_t a, uint32_t b)
+{
+    bf16x8 v;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const auto t = k & 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)(k < 2 ? a : b), 1.0f, true)
+                             : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((int)(k < 2 ? a : b), 1.0f, false);
+        v[2 * k] = t[0];
+        v[2 * k + 1] = t[1];
+    }
+    return v;
+}
+
 // This wave's units of NF unit row blocks that follow each other (wave, wave + 4, ... along the columns; w: the first one's first
 // bytes plus the lane's), in flight.
 template <int NF>
 struct FewUnits {
-    static constexpr int DEPTH = kF8FewDepth / NF;
+    static constexpr int DEPTH = kF8FewDepth;
     u32x4_t u[DEPTH][NF][2];
     const uint8_t *w;
     size_t block;  // bytes of a row block
@@ -88,6 +103,40 @@ struct FewUnits {
 #pragma unroll
         for (int d = 0; d < DEPTH; ++d)
             if (d < n) load(d, d);
+    }
+    // As multiply below, for one gate/up row block, with the products' sums as exact as fp32 sums are (ts: token scales, ws: gate scales, then
+    // up scales, in LDS).  The activations are rounded to 8 bits afterwards: an error of the sums moves some of them across the middle
+    // between two e4m3 values, by 6 to 12 % of the value.  The 8-bit instruction leaves 1.4e-5 (it adds products to 13 bits below the largest
+    // one of a group), which did that to one activation in 5000: layer errors of 1.8e-3 to 6.6e-3 with few tokens where the formula in fp32 has
+    // 1.7e-3.  So here the values are widened to bf16, which is exact, as are their products: 5e-8.  The weights' streaming hides it
+    // (layer of 64 tokens, N=128, I=768, H=2048: 115.0 us, with the 8-bit instruction 116.7; one token 21.3 and 20.3).
+    __device__ __forceinline__ void multiply_widened(uint8_t *lds, int cols, int rows)
+    {
+        static_assert(NF == 1, "");
+        const int lane = threadIdx.x & 63, r = min(lane & (kF8FewRows - 1), rows - 1), half = lane >> 5, nb = cols / kFp8Block;
+        const uint8_t *row = lds + r * few_row(cols) + 16 * half, *ts = lds + kF8FewRows * few_row(cols) + r * nb;
+        const uint8_t *ws = lds + kF8FewRows * (few_row(cols) + nb);
+        f32x16 acc = {};
+        for (int i = 0; i < n; i += DEPTH) {
+#pragma unroll
+            for (int d = 0; d < DEPTH; ++d) {
+                if (i + d >= n) break;
+                const int kb = wave + kF8FewWaves * (i + d);
+                const u32x4_t t[2] = {*reinterpret_cast<const u32x4_t *>(row + kb * 64), *reinterpret_cast<const u32x4_t *>(row + kb * 64 + 32)};
+                f32x16 p = {};
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const u32x4_t wq = u[d][0][q >> 1], tq = t[q >> 1];
+                    const int o = 2 * (q & 1);
+                    p = __builtin_amdgcn_mfma_f32_32x32x16_bf16(few_widen(wq[o], wq[o + 1]), few_widen(tq[o], tq[o + 1]), p, 0, 0, 0);
+                }
+                const int s = (int)ts[kb >> 1] - 254, sg = s + ws[kb >> 1], su = s + ws[nb + (kb >> 1)];
+#pragma unroll
+                for (int k = 0; k < 16; ++k) acc[k] += __builtin_amdgcn_ldexpf(p[k], k < 8 ? sg : su);  // (unit rows 8 (k / 4) ..: gate, then up)
+                if (i + d + DEPTH < n) load(d, i + d + DEPTH);
+            }
+        }
+        leave(lds, &acc);
     }
     // Their products with the LDS rows (those past `rows` repeat the last one); ws: the weights' scales of this lane's row.  The waves'
     // sums take the rows' place: part[block][wave][q][l] = unit rows 8 q + 4 (l / 32) .. + 3, token row l % 32.
@@ -115,6 +164,11 @@ struct FewUnits {
                 if (i + d + DEPTH < n) load(d, i + d + DEPTH);
             }
         }
+        leave(lds, acc);
+    }
+    __device__ __forceinline__ void leave(uint8_t *lds, const f32x16 *acc)
+    {
+        const int lane = threadIdx.x & 63;
         __syncthreads();
         f32x4 *part = reinterpret_cast<f32x4 *>(lds);
 #pragma unroll
@@ -145,7 +199,7 @@ struct FewArgs {
 };
 
 template <int FROM>
-__global__ __launch_bounds__(kF8FewThreads) void fp8_few_gateup_kernel(FewArgs a)
+__global__ __launch_bounds__(kF8FewThreads, 4) void fp8_few_gateup_kernel(FewArgs a)
 {
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     __shared__ TilePlaceLds<kF8FewRows> s_place;
@@ -170,10 +224,11 @@ __global__ __launch_bounds__(kF8FewThreads) void fp8_few_gateup_kernel(FewArgs a
         const int slot = FROM != kFromTables ? s_place.list[r] : a.sorted_slot[loc.y + r];
         return a.x + (size_t)min(max(slot / a.K, 0), a.T - 1) * a.H;  // (a bad index must not fault)
     });
+    const int nb = a.H / kFp8Block;
+    for (int i = threadIdx.x; i < 2 * nb; i += kF8FewThreads)  // scales of the gate rows, of the up rows
+        lds[kF8FewRows * (few_row(a.H) + nb) + i] = a.ws[(((size_t)loc.x * (a.Ip / kFp8Block) + (ft * NF >> 3)) * 2 + i / nb) * fp8_pitch(a.H) + i % nb];
     __syncthreads();
-    // lanes 0 .. 15 of 32 hold gate rows, the others up rows
-    const uint8_t *ws = a.ws + (((size_t)loc.x * (a.Ip / kFp8Block) + (ft * NF >> 3)) * 2 + ((lane >> 4) & 1)) * fp8_pitch(a.H);
-    units.multiply(lds, a.H, loc.z, ws);
+    units.multiply_widened(lds, a.H, loc.z);
     if (threadIdx.x < 4 * NF * kF8FewRows) {  // a thread: activations 4 f .. + 3 of a token row
         const int r = threadIdx.x / (4 * NF), f = threadIdx.x % (4 * NF), l = r + 32 * (f & 1), q = (f & 3) >> 1;
         const f32x4 g = units.total(lds, f >> 2, q, l), u = units.total(lds, f >> 2, q + 2, l);
