@@ -55,7 +55,7 @@ struct F8Args {
     uint8_t *act, *act_s;  // gate/up's result
     void *y;               // down's
     int16_t *y_exp;
-    int N, K, H, Ip, nft;  // nft: feature tiles
+    int T, N, K, H, Ip, nft;  // nft: feature tiles
     int log_terms;         // down: 2^log_terms >= Ip * 448 * 448
 };
 
@@ -77,6 +77,8 @@ struct F8Kernel {
     const F8Args &a;
     uint8_t *ring, *tab;  // LDS: three chunks of token rows; the rows' scales and the weights'
     int e, row0, rows, ft;
+
+    __device__ __forceinline__ int src_row(int r) const { return GATEUP ? min(max(a.sorted_slot[r] / a.K, 0), a.T - 1) : r; }  // (a bad index must not fault)
 
     template <int NB>
     __device__ __forceinline__ void run() const
@@ -102,7 +104,7 @@ struct F8Kernel {
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
             const int r = row0 + min(32 * b + (tid >> 3), rows - 1);
-            tp[b] = a.src + (size_t)(GATEUP ? a.sorted_slot[r] / a.K : r) * ld + (((tid & 7) ^ ((tid >> 4) & 7)) << 4);
+            tp[b] = a.src + (size_t)src_row(r) * ld + (((tid & 7) ^ ((tid >> 4) & 7)) << 4);
         }
         uint8_t *wtab = tab + kF8Tok * pitch;
         const uint32_t my_ws = lds_addr(wtab + (GATEUP ? l32 >> 4 : wave >> 1) * pitch), my_ts = lds_addr(tab + l32 * pitch);
@@ -187,7 +189,7 @@ struct F8Kernel {
         for (int i = tid; i < NB * 32 * (pitch / 4); i += kF8Threads) {
             const int r = i / (pitch / 4), c = i - r * (pitch / 4), rr = row0 + min(r, rows - 1);
             reinterpret_cast<uint32_t *>(tab)[i] =
-                reinterpret_cast<const uint32_t *>(a.src_s + (size_t)(GATEUP ? a.sorted_slot[rr] / a.K : rr) * pitch)[c];
+                reinterpret_cast<const uint32_t *>(a.src_s + (size_t)src_row(rr) * pitch)[c];
         }
         {
             // (down: a workgroup's 256 rows are two blocks of 128)
@@ -379,7 +381,7 @@ int launch_ffn_fp8(const zeda_layer_desc *d, const void *x, const zeda_fp8_exper
     if (rc != ZEDA_OK) return rc;
     F8Args a = {};
     a.offsets = offsets; a.sorted_slot = sorted_slot;
-    a.N = d->N; a.K = d->K; a.H = d->H; a.Ip = Ip;
+    a.T = d->T; a.N = d->N; a.K = d->K; a.H = d->H; a.Ip = Ip;
     a.src = w + L.x; a.src_s = w + L.xs;
     a.w = (const uint8_t *)e->w_gateup; a.ws = (const uint8_t *)e->s_gateup;
     a.act = w + L.act; a.act_s = w + L.act_s;

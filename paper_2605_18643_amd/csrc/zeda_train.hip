@@ -151,7 +151,11 @@ static TrainWs train_ws(const zeda_layer_desc *d)
     TrainWs w;
     size_t o = 0;
     auto take = [&](size_t bytes) { const size_t at = o; o += align_up(bytes ? bytes : 1, 256); return at; };
-    w.tables = take(route_train_fused(d) ? 0 : route_tables(d).bytes());
+    // (callers size workspaces once, for their longest batch: never less for a longer one, whose router may need no tables.  A split has at
+    // most eight slices and 4096 tokens times slices, whatever the batch)
+    const RouteTables t = route_tables(d);
+    const size_t rows = (size_t)ceil_div(d->T, 32) * 256;
+    w.tables = take(d->dtype == ZEDA_BF16 ? (rows < 4096 ? rows : 4096) * t.E * 4 : t.bytes());
     w.part_p = take(nblk * NE * 4);
     w.part_c = take(nblk * (NE + 1) * 4);
     w.done = take(4);
@@ -592,7 +596,7 @@ static BackWs back_ws(const zeda_layer_desc *d)
     const int most = ceil_div(w.Tp, 128);
     if (splits > most) splits = most;
     w.per = splits ? ceil_div(most, splits) * 128 : 128;
-    w.splits = ceil_div(w.Tp, w.per);
+    w.splits = ceil_div(w.Tp, w.per);  // (at most `splits`, which does not fall as T grows: the scratch is sized by that)
     size_t o = 0;
     auto take = [&](size_t bytes) { const size_t at = o; o += align_up(bytes ? bytes : 1, 256); return at; };
     const size_t n = (size_t)w.Tp * w.NEp * es;
@@ -600,7 +604,7 @@ static BackWs back_ws(const zeda_layer_desc *d)
     w.cols = take(n * (es == 2 ? 3 : 1));
     w.part_b = take((size_t)w.nblk * NE * 4);
     w.on = take((size_t)w.nblk * 4);
-    w.part = take((size_t)w.splits * w.NE16 * d->H * 4);
+    w.part = take((size_t)splits * w.NE16 * d->H * 4);
     w.total = o;
     return w;
 }

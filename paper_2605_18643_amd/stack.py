@@ -32,7 +32,7 @@ class MoeStack:
             if tiled:
                 wg, wu, wd = zeda.zeda_pack_expert_weights(zeda.make_desc(w.T, w.H, w.I, w.N, 0, w.K, w.dtype), wg, wu, wd)
             if fp8:
-                d = zeda.make_desc(w.T, w.H, w.I, w.N, 0, w.K, w.dtype)
+                d = zeda.make_desc(w.T, w.H, w.I, w.N, 0, 1, w.dtype)  # (the experts' shapes alone matter)
                 experts = zeda.zeda_pack_expert_weights_fp8(d, *[t for m in (wg, wu, wd) for t in zeda.zeda_quantize_weights_fp8(m)])
                 self.weights.append({"w_router": wr, "router_bias": bias, "experts": experts})
             else:
@@ -82,7 +82,7 @@ class MoeStack:
         before the residual add."""
         if fused is None:
             fused = hook is None
-        ids = zeda.ws_views(self.desc, self.ws)["topk_ids"] if token_zero is not None else None  # (at the start of every workspace)
+        ids = zeda.ws_views(self.desc, self.ws, self.fp8)["topk_ids"] if token_zero is not None else None
         layer = zeda.zeda_moe_forward_fp8 if self.fp8 else zeda.zeda_moe_forward
         block = zeda.zeda_moe_block_forward_fp8 if self.fp8 else zeda.zeda_moe_block_forward
         if fused:

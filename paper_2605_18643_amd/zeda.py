@@ -264,6 +264,10 @@ def zeda_moe_block_forward(desc, xn, x_res, w_router, router_bias, w_gate, w_up,
                                         _stream(stream)), "zeda_moe_block_forward")
 
 
+def _dtype_of(desc: LayerDesc) -> torch.dtype:
+    return torch.bfloat16 if desc.dtype == ZEDA_BF16 else torch.float32
+
+
 def _dtype_code(t: torch.Tensor) -> int:
     return ZEDA_BF16 if t.dtype == torch.bfloat16 else ZEDA_F32
 
@@ -430,10 +434,24 @@ def route_backward_workspace_bytes(desc: LayerDesc) -> int:
     return int(lib().zeda_route_backward_workspace_bytes(ctypes.byref(desc)))
 
 
+def _typed(where: str, *args) -> None:
+    """(tensor or None, type, elements): types and sizes that the C side cannot see of a pointer."""
+    for t, dtype, n in args:
+        _need(t is None or (t.dtype == dtype and t.numel() >= n and t.is_contiguous()), where)
+
+
+def _token_mask(mask, T: int, where: str) -> None:
+    _need(mask is None or (mask.dtype in (torch.uint8, torch.bool) and mask.numel() == T and mask.is_contiguous()), where)
+
+
 def zeda_route_train(desc, x, w_router, router_bias, token_mask, alpha: float, w: float, topk_ids, topk_gates, probs, counts, mean_probs, summary,
                      ws, stream=None) -> None:
     """zeda_route that also leaves probs[T, N+Z], and over the tokens with token_mask (uint8[T] or None) != 0 counts[N+Z], mean_probs[N+Z] and
     summary[7] (as zeda_routing_stats: the balance losses are summary[5] and summary[6])."""
+    S, NE, f = desc.T * desc.K, desc.N + desc.Z, torch.float32
+    _token_mask(token_mask, desc.T, "zeda_route_train")
+    _typed("zeda_route_train", (x, _dtype_of(desc), desc.T * desc.H), (w_router, _dtype_of(desc), NE * desc.H), (router_bias, f, NE), (topk_ids, torch.int32, S),
+           (topk_gates, f, S), (probs, f, desc.T * NE), (counts, torch.int32, NE), (mean_probs, f, NE), (summary, f, 7))
     _check(lib().zeda_route_train(ctypes.byref(desc), _ptr(x), _ptr(w_router), _ptr(router_bias), _ptr(token_mask), float(alpha), float(w),
                                   _ptr(topk_ids), _ptr(topk_gates), _ptr(probs), _ptr(counts), _ptr(mean_probs), _ptr(summary), _ptr(ws),
                                   ws.numel() * ws.element_size(), _stream(stream)), "zeda_route_train")
@@ -442,6 +460,10 @@ def zeda_route_train(desc, x, w_router, router_bias, token_mask, alpha: float, w
 def zeda_route_backward(desc, x, w_router, probs, topk_ids, topk_gates, token_mask, counts, alpha: float, w: float, d_loss, d_gates, dx, dw_router,
                         dbias, ws, stream=None) -> None:
     """Gradients of d_loss[0] L_A + d_loss[1] L_GA + <d_gates, topk_gates>: dx (type of x), dw_router and dbias (fp32); each may be None."""
+    S, NE, f, dt = desc.T * desc.K, desc.N + desc.Z, torch.float32, _dtype_of(desc)
+    _token_mask(token_mask, desc.T, "zeda_route_backward")
+    _typed("zeda_route_backward", (x, dt, desc.T * desc.H), (w_router, dt, NE * desc.H), (probs, f, desc.T * NE), (topk_ids, torch.int32, S), (topk_gates, f, S),
+           (counts, torch.int32, NE), (d_loss, f, 2), (d_gates, f, S), (dx, dt, desc.T * desc.H), (dw_router, f, NE * desc.H), (dbias, f, NE))
     _check(lib().zeda_route_backward(ctypes.byref(desc), _ptr(x), _ptr(w_router), _ptr(probs), _ptr(topk_ids), _ptr(topk_gates), _ptr(token_mask),
                                      _ptr(counts), float(alpha), float(w), _ptr(d_loss), _ptr(d_gates), _ptr(dx), _ptr(dw_router), _ptr(dbias),
                                      _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)), "zeda_route_backward")
@@ -449,13 +471,17 @@ def zeda_route_backward(desc, x, w_router, probs, topk_ids, topk_gates, token_ma
 
 def zeda_combine_backward(desc, d_out, y_slot, topk_ids, topk_gates, slot_to_row, x, d_gates, d_y_slot, dx, stream=None) -> None:
     """Backward of zeda_combine.  d_y_slot may be None; x and dx belong to EXPERT_COPY (None otherwise, dx None if not wanted)."""
+    S, f, dt = desc.T * desc.K, torch.float32, _dtype_of(desc)
+    _typed("zeda_combine_backward", (d_out, dt, desc.T * desc.H), (topk_ids, torch.int32, S), (topk_gates, f, S), (slot_to_row, torch.int32, S),
+           (x, dt, desc.T * desc.H), (d_gates, f, S), (d_y_slot, dt, S * desc.H), (dx, dt, desc.T * desc.H))
     _check(lib().zeda_combine_backward(ctypes.byref(desc), _ptr(d_out), _ptr(y_slot), _ptr(topk_ids), _ptr(topk_gates), _ptr(slot_to_row), _ptr(x),
                                        _ptr(d_gates), _ptr(d_y_slot), _ptr(dx), _stream(stream)), "zeda_combine_backward")
 
 
-def ws_views(desc: LayerDesc, ws: torch.Tensor):
-    """Typed views of the intermediate results zeda_moe_forward leaves in its workspace."""
-    L = workspace_layout(desc)
+def ws_views(desc: LayerDesc, ws: torch.Tensor, fp8: bool = False):
+    """Typed views of the intermediate results zeda_moe_forward leaves in its workspace (fp8: zeda_moe_forward_fp8, whose
+    activations and expert outputs are in forms of the kernels' own: only the routing)."""
+    L = workspace_layout_fp8(desc) if fp8 else workspace_layout(desc)
     S = desc.T * desc.K
     dt = torch.bfloat16 if desc.dtype == ZEDA_BF16 else torch.float32
     es = 2 if desc.dtype == ZEDA_BF16 else 4
@@ -464,13 +490,15 @@ def ws_views(desc: LayerDesc, ws: torch.Tensor):
     def view(off, n, dtype, size):
         return b[off: off + n * size].view(dtype)
 
-    return {
+    views = {
         "topk_ids": view(L.topk_ids, S, torch.int32, 4).view(desc.T, desc.K),
         "topk_gates": view(L.topk_gates, S, torch.float32, 4).view(desc.T, desc.K),
         "expert_offsets": view(L.expert_offsets, desc.N + 1, torch.int32, 4),
         "sorted_slot": view(L.sorted_slot, S, torch.int32, 4),
         "slot_to_row": view(L.slot_to_row, S, torch.int32, 4),
         "num_real": view(L.num_real, 1, torch.int32, 4),
-        "act": view(L.act, S * desc.I, dt, es).view(S, desc.I),
-        "y_slot": view(L.y_slot, S * desc.H, dt, es).view(S, desc.H),
     }
+    if not fp8:
+        views["act"] = view(L.act, S * desc.I, dt, es).view(S, desc.I)
+        views["y_slot"] = view(L.y_slot, S * desc.H, dt, es).view(S, desc.H)
+    return views

@@ -121,3 +121,10 @@ def test_binding_refuses_what_the_library_cannot_see():
         with pytest.raises(zeda.ZedaError) as err:
             f()
         assert err.value.status == EINVAL
+
+
+def test_a_longer_batch_never_needs_less():
+    for kw in (dict(), dict(N=64, I=1536, K=4), dict(N=12, I=192, H=256, K=2), dict(N=2, Z=0, I=64, H=128, K=1)):
+        sizes = [zeda.expert_ffn_workspace_bytes_fp8(zeda.make_desc(**{**dict(T=T, H=2048, I=768, N=128, Z=32, K=8, dtype="bf16"), **kw}))
+                 for T in list(range(1, 300)) + list(range(301, 20000, 97))]
+        assert all(a <= b for a, b in zip(sizes, sizes[1:])), kw

@@ -333,6 +333,34 @@ def test_tiles_of_all_sizes_keep_their_bits_after_other_data(H, I):
         assert torch.equal(run(x), first), rep
 
 
+def test_a_slot_out_of_range_is_some_token():
+    """Rows of one expert whose slots do not exist (few rows and a tile's worth): the other experts' rows are what they were."""
+    for loads in ([3, 5], [300, 900, 1000, 700]):
+        T, N = sum(loads), len(loads)
+        w, d = _layer(T, 256, 192, N, 1, 1)
+        qs = [zeda.zeda_quantize_weights_fp8(m.contiguous()) for m in synth.draw_experts(w, "cuda")]
+        packed, x = zeda.zeda_pack_expert_weights_fp8(d, *[t for p in qs for t in p]), synth.draw_tokens(w, "cuda")
+        off, ss, _, nr = _dispatch(d, torch.tensor(np.repeat(np.arange(N), loads), dtype=torch.int32, device="cuda").view(T, 1))
+        ws = torch.empty(zeda.expert_ffn_workspace_bytes_fp8(d), dtype=torch.uint8, device="cuda")
+        want, got = (torch.empty(T, 256, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        zeda.zeda_expert_ffn_fp8(d, x, packed, off, ss, nr, want, ws)
+        ss[: loads[0]] = torch.tensor([2 ** 31 - 1, -(2 ** 31), T], dtype=torch.int32, device="cuda").repeat(loads[0] // 3)
+        zeda.zeda_expert_ffn_fp8(d, x, packed, off, ss, nr, got, ws)
+        torch.cuda.synchronize()
+        assert torch.equal(got[loads[0]:], want[loads[0]:])
+
+
+def test_stack_whose_workspace_is_smaller_than_the_bf16_layers():
+    """The ids for the per-token counters lie where the 8-bit layout says; views by the bf16 layout would end past it."""
+    w, d = _layer(3000, 128, 1024, 3, 3, 4)
+    assert zeda.workspace_bytes_fp8(d) < zeda.workspace_layout(d).y_slot + 3000 * 4 * 128 * 2
+    stack = MoeStack(w, 2, fp8=True)
+    zero = torch.zeros(3000, dtype=torch.int32, device="cuda")
+    stack.forward(synth.draw_tokens(w, "cuda"), token_zero=zero)
+    torch.cuda.synchronize()
+    assert int(zero.sum()) == 2 * 3000 * 4 - int(stack.num_real.sum())
+
+
 @pytest.mark.parametrize("T", [1, 24, 333])
 def test_residual_block_and_stack(T):
     w, d = _layer(T, 256, 192, 6, 3, 3)

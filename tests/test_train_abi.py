@@ -2,6 +2,7 @@
 import ctypes
 
 import pytest
+import torch
 
 from paper_2605_18643_amd import zeda
 
@@ -91,3 +92,37 @@ def test_outputs_over_inputs_are_refused():
         assert _combine(copy, dx=A[o]) == EINVAL, o
     assert _combine(copy, dy=A["x"]) == EINVAL
     assert _combine(_desc(T=0)) == OK
+
+
+def test_a_longer_batch_never_needs_less():
+    """Workspaces are sized once, for the longest batch."""
+    for kw in (dict(), dict(N=64, K=4), dict(H=1024, N=12, Z=4, K=3), dict(H=7168, N=250, Z=6), dict(dtype="f32", H=1152)):
+        for size in (zeda.route_train_workspace_bytes, zeda.route_backward_workspace_bytes):
+            sizes = [size(_desc(T=T, **kw)) for T in list(range(0, 300)) + list(range(301, 20000, 97))]
+            assert all(a <= b for a, b in zip(sizes, sizes[1:])), (kw, size.__name__)
+
+
+def test_tensors_of_another_type_or_size_are_refused():
+    """What a pointer does not say."""
+    d = _desc(T=6, H=128, N=3, Z=2, K=2)
+    f, i = torch.float32, torch.int32
+    shapes = dict(x=((6, 128), torch.bfloat16), wr=((5, 128), torch.bfloat16), ids=((6, 2), i), gates=((6, 2), f), probs=((6, 5), f), counts=((5,), i), P=((5,), f),
+                  summary=((7,), f), ws=((64,), torch.uint8), mask=((6,), torch.uint8), d_loss=((2,), f), d_gates=((6, 2), f), dx=((6, 128), torch.bfloat16),
+                  dw=((5, 128), f), dbias=((5,), f), d_out=((6, 128), torch.bfloat16), y=((12, 128), torch.bfloat16), s2r=((12,), i), dy=((12, 128), torch.bfloat16))
+    t = {n: torch.zeros(s, dtype=k) for n, (s, k) in shapes.items()}
+
+    def calls(**kw):
+        a = {**t, **kw}
+        return (lambda: zeda.zeda_route_train(d, a["x"], a["wr"], None, a["mask"], 0.01, 2.0, a["ids"], a["gates"], a["probs"], a["counts"], a["P"], a["summary"], a["ws"]),
+                lambda: zeda.zeda_route_backward(d, a["x"], a["wr"], a["probs"], a["ids"], a["gates"], a["mask"], a["counts"], 0.01, 2.0, a["d_loss"],
+                                                 a["d_gates"], a["dx"], a["dw"], a["dbias"], a["ws"]),
+                lambda: zeda.zeda_combine_backward(d, a["d_out"], a["y"], a["ids"], a["gates"], a["s2r"], None, a["d_gates"], a["dy"], None))
+
+    for which, names in enumerate((("x", "wr", "mask", "ids", "gates", "probs", "counts", "P", "summary"),
+                                   ("x", "wr", "mask", "probs", "ids", "gates", "counts", "d_loss", "d_gates", "dx", "dw", "dbias"),
+                                   ("d_out", "ids", "gates", "s2r", "d_gates", "dy"))):
+        for n in names:
+            for bad in (t[n].to(torch.float64), t[n][:-1]):
+                with pytest.raises(zeda.ZedaError) as e:
+                    calls(**{n: bad})[which]()
+                assert e.value.status == EINVAL, n
