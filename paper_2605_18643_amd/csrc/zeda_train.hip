@@ -202,7 +202,7 @@ int launch_route_train(const zeda_layer_desc *d, const void *x, const void *wr, 
 // does not change when a constant is added to a: the slopes' mean is taken off, in 64 bits, so that what they differ
 // by is kept.  Gates: SOFTMAX adds dg_j to a at the selected experts; the normalised forms add g_j (dg_j - s), s = sum_l dg_l g_l,
 // on the experts of the denominator and g_j dg_j on a selected expert outside it.
-constexpr int kBackTokens = 32, kBackThreads = 512;
+constexpr int kBackTokens = 32, kBackThreads = 1024;
 
 // bf16 parts by truncation: v = v0 + v1 + v2 exactly (24 bits)
 __device__ __forceinline__ uint16_t top_bits(float v) { return (uint16_t)(__float_as_uint(v) >> 16); }
@@ -222,7 +222,7 @@ struct LogitGrad {
     int Tp, NEp;
 };
 
-// A wave takes four tokens, lane l the experts l, l + 64, ...  F32: both copies in fp32; else the rows as two bf16 parts (their
+// A wave takes two tokens, lane l the experts l, l + 64, ...  F32: both copies in fp32; else the rows as two bf16 parts (their
 // product is rounded to bf16), the columns as three (theirs stays fp32: nothing of dl is lost).  on[block]: which of the block's
 // tokens count, a bit each.
 template <bool F32>
@@ -270,7 +270,7 @@ __global__ __launch_bounds__(kBackThreads) void logit_grad_kernel(LogitGrad a)
             s_a[lane + 64 * q] = (float)(kA / NE * ((double)c[q] * NE - (cE + cZ)) + (lane + 64 * q < N ? apart * (NE - N) : -apart * N));
     }
     __syncthreads();
-    // (the tokens side by side: each step is a broadcast from one lane and four comparisons)
+    // (a wave's tokens side by side: each step is a broadcast from one lane and four comparisons)
     float u[PER][4], g_of[PER][4] = {}, v_of[PER][4] = {}, sum[PER] = {};
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
@@ -375,10 +375,9 @@ __device__ __forceinline__ void turn8x4(const uint2 (&r)[8], bf16x8 (&c)[4])
 
 // dx[T, H] = dl w_router.  A wave keeps its 64 columns of w_router (all experts) in registers and walks over 16-token blocks.
 // Lane (l16, kq) of a 16x16x32 product: columns 4 l16 .. + 3 as four operands, experts 8 kq .. + 7 of the step.
-constexpr int kDxTokens = 128;
 template <int KS>  // steps of 32 experts
 __global__ __launch_bounds__(256) void router_dx_bf16_kernel(const uint16_t *__restrict__ dl, const bf16_t *__restrict__ wr, int T, int H, int NE,
-                                                             int Tp, bf16_t *__restrict__ dx)
+                                                             int Tp, int per, bf16_t *__restrict__ dx)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, kq = lane >> 4;
     const int h0 = (blockIdx.y * 4 + wave) * 64;
@@ -394,17 +393,17 @@ __global__ __launch_bounds__(256) void router_dx_bf16_kernel(const uint16_t *__r
         }
         turn8x4(r, wf[k]);
     }
-    const int tb = min(T, (int)(blockIdx.x + 1) * kDxTokens);
+    const int ta = blockIdx.x * per, tb = min(T, ta + per);
     const size_t plane = (size_t)Tp * KS * 32;
-    bf16x8 df[2][KS];
-    auto fetch = [&](int t0) {
+    // dl of the next two token blocks is on its way while one is multiplied
+    bf16x8 df[2][2][KS];
+    auto fetch = [&](bf16x8 (&to)[2][KS], int t0) {
 #pragma unroll
         for (int q = 0; q < 2; ++q)
 #pragma unroll
-            for (int k = 0; k < KS; ++k) df[q][k] = *reinterpret_cast<const bf16x8 *>(dl + q * plane + ((size_t)(t0 >> 4) * KS + k) * 512 + l16 * 32 + 8 * kq);
+            for (int k = 0; k < KS; ++k) to[q][k] = *reinterpret_cast<const bf16x8 *>(dl + q * plane + ((size_t)(t0 >> 4) * KS + k) * 512 + l16 * 32 + 8 * kq);
     };
-    fetch(blockIdx.x * kDxTokens);
-    for (int t0 = blockIdx.x * kDxTokens; t0 < tb; t0 += 16) {
+    auto block = [&](bf16x8 (&d)[2][KS], int t0) {
         f32x4 acc[4];
 #pragma unroll
         for (int c = 0; c < 4; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -413,8 +412,8 @@ __global__ __launch_bounds__(256) void router_dx_bf16_kernel(const uint16_t *__r
 #pragma unroll
             for (int k = 0; k < KS; ++k)
 #pragma unroll
-                for (int c = 0; c < 4; ++c) acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(df[q][k], wf[k][c], acc[c], 0, 0, 0);
-        if (t0 + 16 < tb) fetch(t0 + 16);
+                for (int c = 0; c < 4; ++c) acc[c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(d[q][k], wf[k][c], acc[c], 0, 0, 0);
+        if (t0 + 32 < tb) fetch(d, t0 + 32);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int t = t0 + 4 * kq + i;
@@ -423,6 +422,12 @@ __global__ __launch_bounds__(256) void router_dx_bf16_kernel(const uint16_t *__r
             for (int c = 0; c < 4; ++c) v[c] = (bf16_t)acc[c][i];
             if (t < T) *reinterpret_cast<bf16x4 *>(dx + (size_t)t * H + h0 + 4 * l16) = v;
         }
+    };
+    fetch(df[0], ta);
+    if (ta + 16 < tb) fetch(df[1], ta + 16);
+    for (int t0 = ta; t0 < tb; t0 += 32) {
+        block(df[0], t0);
+        if (t0 + 16 < tb) block(df[1], t0 + 16);
     }
 }
 
@@ -645,8 +650,12 @@ int launch_route_backward(const zeda_layer_desc *d, const void *x, const void *w
                 router_dx_f32_kernel<<<dim3(L.Tp / 64, ceil_div(H, 256)), 256, 0, s>>>((const float *)(b + L.rows), (const float *)wr, d->T, H, NE, L.NEp,
                                                                                    (float *)dx);
             } else {
-                const dim3 grid(ceil_div(d->T, kDxTokens), ceil_div(H, 256));
-#define ZEDA_DX(KS) router_dx_bf16_kernel<KS><<<grid, 256, 0, s>>>((const uint16_t *)(b + L.rows), (const bf16_t *)wr, d->T, H, NE, L.Tp, (bf16_t *)dx)
+                // Tokens of a workgroup: as many workgroups as run at once (two to a CU), from 32 up (each fetches its part of w_router), and no more
+                // than 128 to a workgroup, which leaves the last round fuller.  H = 2048, us, always 128 / so: 200 tokens 10.8 / 4.4, 997 8.9 / 4.4,
+                // 2048 11.2 / 8.6, 4096 12.8 / 12.6, 8192 18.1 / 18.2 (twice as many workgroups there: 21.0)
+                const int even = ceil_div((int)((int64_t)d->T * ceil_div(H, 256) / 512), 32) * 32, per = even < 32 ? 32 : even > 128 ? 128 : even;
+                const dim3 grid(ceil_div(d->T, per), ceil_div(H, 256));
+#define ZEDA_DX(KS) router_dx_bf16_kernel<KS><<<grid, 256, 0, s>>>((const uint16_t *)(b + L.rows), (const bf16_t *)wr, d->T, H, NE, L.Tp, per, (bf16_t *)dx)
                 switch (L.NEp / 32) {
                     case 1: ZEDA_DX(1); break; case 2: ZEDA_DX(2); break; case 3: ZEDA_DX(3); break; case 4: ZEDA_DX(4); break;
                     case 5: ZEDA_DX(5); break; case 6: ZEDA_DX(6); break; case 7: ZEDA_DX(7); break; default: ZEDA_DX(8); break;
