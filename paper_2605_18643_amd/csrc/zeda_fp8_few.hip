@@ -5,6 +5,8 @@
 // the matrix instruction.  The token rows are rounded to 8 bits by every workgroup for itself, into LDS, while its weights are
 // on their way: x in gate/up, the fp32 activations that gate/up leaves in down, whose 128-column blocks span eight workgroups.
 // No launch for a quantisation is left, and for short calls none for placement and selection (zeda_place.h).
+// HBM-bound: N=128, I=768, H=2048, 64 tokens (106 experts hit): gate/up 62.8 us = 5.3 TB/s, down 37.6 us = 4.4 TB/s; one token with four real
+// slots 10.0 and 5.1 us, a chain of latencies (placement, weights, join of the waves' sums).
 #include <type_traits>
 
 #include "zeda_fp8.h"
