@@ -266,7 +266,7 @@ int zeda_moe_block_forward(const zeda_layer_desc *desc, const void *xn, void *x_
  * where G, U, D are stored under one scale per 128 x 128 block.  Sums are fp32; in G xq and U xq of small batches as exact as fp32 is, else
  * with the products' bits that the 8-bit matrix instruction keeps, within about 13 binades of the largest product of a group:
  * relative to the root mean square of a sum that is 1.4e-5, which moves one activation in some thousands to the neighbouring e4m3
- * value (the result is then 2.0e-3 off the formula, against 1.7e-3 for the rounding to bf16 alone).  h is rounded once, from fp32.  An infinity or
+ * value (the result is then about 2.0e-3 off the formula, against 1.7e-3 for the rounding to bf16 alone).  h is rounded once, from fp32.  An infinity or
  * no-number in x or h becomes a no-number and makes the token's expert outputs no-numbers; other tokens are not affected.
  * Routing, dispatch, combine, x, the router and the result are those of the bf16 layer: desc->dtype must be ZEDA_BF16, and
  * H and I at most 16384 (ZEDA_EUNSUPPORTED otherwise); desc->weight_layout is ignored.

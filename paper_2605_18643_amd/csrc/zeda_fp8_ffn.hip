@@ -2,16 +2,19 @@
 //   xq = Q(x), h = silu(G xq) .* (U xq), y = D Q(h),
 // Q = rounding to e4m3 under a power-of-two scale for every 128 columns, G, U, D e4m3 under one for every 128 x 128 block.
 //
-// Tiles of up to 128 token rows x 256 weight rows.  Every weight byte is used by one wave only, so weights go straight into the registers
-// of the matrix instruction (their layout is its operand's, 2 KiB a fetch); token rows, which all four waves use, go through a ring of
-// three chunks in LDS.  The scales ride along as operands of the instruction (bytes of powers of two).  Two workgroups to a CU: one's
-// prologue and epilogue run under the other's products.
+// Tiles of up to 160 token rows x 256 weight rows.  Every weight byte is used by one wave only, so weights go straight into the registers
+// of the matrix instruction (their layout is its operand's, 2 KiB a fetch), half a chunk of 128 columns at a time into the registers that
+// the products before have freed; token rows, which all four waves use, go through a ring of three chunks in LDS.  The scales ride
+// along as operands of the instruction (bytes of powers of two).  Two workgroups to a CU: one's prologue and epilogue run under the
+// other's products.
 // What bounds it: with up to 128 rows an expert the weights from HBM (997 tokens, N=64, I=1536, H=2048: gate/up 403 MB in 77 us = 5.2 TB/s, the
-// rate of a large copy); at 4096 tokens of N=128, I=768, whose experts have 128 rows on average, every second expert needs a second tile
-// of a few rows, and gate/up takes 115 us, down 65; with thousands of rows the fetches out of L2 (13 TB/s) and the products, which take
-// turns rather than overlap: 16381 skewed tokens 190-298 us and 137-218 us by the run's clock, matrix pipes busy 44 % of the cycles.
-// Tried and slower: one workgroup of eight waves with 192-row tiles and two chunks ahead (gate/up at 4096 tokens 118 -> 105 us, but 258 ->
-// 305 at 16381, and down), one of four waves with twice the accumulators (4096 tokens, whole layer: 219 -> 320 us).
+// rate of a large copy).  4096 tokens of N=128, I=768 have 128 rows an expert on average, so every second expert of its tiles of 128 needs a
+// second one: gate/up 103 us, down 64; 16381 skewed tokens 167-271 and 123-199 us by the run's clock, the matrix pipes busy 53 and 33 % of the
+// cycles (down writes 16 bits a product of 768 terms).
+// What the compiler must not see as flat: token rows fetched by global loads into LDS made it wait for everything in flight before the first
+// product of every chunk (4096 tokens, whole layer, 205 us against 202; 8192 tokens 283 against 270; 16381 470 against 444).
+// Tried and slower: one workgroup of eight waves with 192-row tiles and two chunks ahead (16381 tokens: gate/up 258 -> 305 us), one of four
+// waves with twice the accumulators (4096 tokens, whole layer: 219 -> 320 us).
 //
 // Sums: the matrix instruction adds its products with the bits down to 2^-13 of the largest of a group: 1.4e-5 of a sum's root mean square.
 // That moves one activation in 5000 to the next 8-bit value and puts the layer's result 2.0e-3 off where fp32 sums and the rounding of the
@@ -26,21 +29,22 @@
 
 namespace zeda {
 
-constexpr int kF8Tok = 128;      // token rows of a tile
+constexpr int kF8Tok = 160;      // token rows of a tile at most
 constexpr int kF8Threads = 256;  // four waves, each two units (64 rows) of the weights against all token rows of the tile
 
 // One wave: {expert, first row, rows} of token tile `tile` of the expert-sorted rows, and the number of tiles of all experts.
 struct F8Tiles {
-    int off[5], nt[4], excl, total;
-    __device__ __forceinline__ void count(const int32_t *__restrict__ offsets, int N)
+    int off[5], nt[4], excl, total, tok;
+    __device__ __forceinline__ void count(const int32_t *__restrict__ offsets, int N, int rows)
     {
         const int lane = threadIdx.x & 63;
         int local = 0;
+        tok = rows;
 #pragma unroll
         for (int q = 0; q < 5; ++q) off[q] = offsets[min(4 * lane + q, N)];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            nt[q] = (off[q + 1] - off[q] + kF8Tok - 1) / kF8Tok;
+            nt[q] = (off[q + 1] - off[q] + tok - 1) / tok;
             local += nt[q];
         }
         const int incl = wave_scan(local);
@@ -54,8 +58,8 @@ struct F8Tiles {
         for (int q = 0; q < 4; ++q) {
             if (tile >= at && tile < at + nt[q]) {
                 e = 4 * (threadIdx.x & 63) + q;
-                row0 = off[q] + (tile - at) * kF8Tok;
-                rows = min(kF8Tok, off[q + 1] - row0);
+                row0 = off[q] + (tile - at) * tok;
+                rows = min(tok, off[q + 1] - row0);
             }
             at += nt[q];
         }
@@ -71,7 +75,7 @@ struct F8Args {
     uint8_t *act, *act_s;  // gate/up's result
     void *y;               // down's
     int16_t *y_exp;
-    int T, N, K, H, Ip, nft;  // nft: feature tiles
+    int T, N, K, H, Ip, tok, nft;  // token rows of a tile, feature tiles
     int log_terms;         // down: 2^log_terms >= Ip * 448 * 448
 };
 
@@ -87,7 +91,7 @@ constexpr int kF8Slot = kF8Tok * kFp8Block, kF8Ring = 3 * kF8Slot;
 template <typename F, int... S>
 __device__ __forceinline__ void for_steps(F &f, std::integer_sequence<int, S...>) { (f(std::integral_constant<int, S>{}), ...); }
 
-template <int KIND, int ODD>  // ODD: the number of chunks is odd
+template <int KIND, bool ONE, bool BIG>  // ONE: a single chunk; BIG: token rows past 4 GiB
 struct F8Kernel {
     static constexpr bool GATEUP = KIND == kF8GateUp;
     const F8Args &a;
@@ -106,22 +110,26 @@ struct F8Kernel {
         const uint8_t *wp[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) wp[u] = a.w + ((size_t)e * rbs + min(rb + u, rbs - 1)) * (2 * nk) * kFp8Unit;
-        u32x4 wa[2][2][4];
-        auto load_w = [&](u32x4 (&d)[2][4], int c) {
+        u32x4 w[2][4];
+        auto load_w = [&](int c, int m) {  // half m of chunk c's columns
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) d[u][q] = *reinterpret_cast<const u32x4 *>(wp[u] + (size_t)c * (2 * kFp8Unit) + q * 1024 + lane * 16);
+                for (int q = 2 * m; q < 2 * m + 2; ++q) w[u][q] = *reinterpret_cast<const u32x4 *>(wp[u] + (size_t)c * (2 * kFp8Unit) + q * 1024 + lane * 16);
         };
-        load_w(wa[0], 0);  // (what an item starts from is asked for before anything waits: weights, token rows, scales)
+        load_w(0, 0);
+        load_w(0, 1);  // (what an item starts from is asked for before anything waits: weights, token rows, scales)
         // This thread's piece of the token rows of every 32-row block: row tid / 8, and the ring's position tid % 8 of that row, where
         // the row's 16-byte pieces stand permuted by the row: 16 lanes that read one piece of 16 rows touch all banks once.
-        const uint8_t *tp[NB];
+        // They are fetched by buffer loads with 32-bit offsets (gate/up: into all tokens; down: into the tile's rows): a global load into LDS
+        // counts as flat with the compiler, which then waits for everything in flight wherever it needs a weight.
+        std::conditional_t<BIG, size_t, uint32_t> tp[NB];
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
-            const int r = row0 + min(32 * b + (tid >> 3), rows - 1);
-            tp[b] = a.src + (size_t)src_row(r) * ld + (((tid & 7) ^ ((tid >> 4) & 7)) << 4);
+            const int r = min(32 * b + (tid >> 3), rows - 1);
+            tp[b] = (std::conditional_t<BIG, size_t, uint32_t>)(GATEUP ? src_row(row0 + r) : r) * ld + (((tid & 7) ^ ((tid >> 4) & 7)) << 4);
         }
+        const __amdgpu_buffer_rsrc_t rsrc = __builtin_amdgcn_make_buffer_rsrc((void *)(GATEUP ? a.src : a.src + (size_t)row0 * ld), 0, 0xffffffff, 0x00027000);
         uint8_t *wtab = tab + kF8Tok * pitch;
         const uint32_t my_ws = lds_addr(wtab + (GATEUP ? l32 >> 4 : wave >> 1) * pitch), my_ts = lds_addr(tab + l32 * pitch);
 
@@ -133,18 +141,19 @@ struct F8Kernel {
 #pragma unroll
                 for (int i = 0; i < 16; ++i) acc[u][b][i] = 0.f;
 
-        // Per chunk of 128 columns a wave fetches its weights into registers, one chunk ahead, and a quarter of the token rows
-        // into the ring, two chunks ahead.  Loads return in order, so a wave that has used chunk c's weights has the token rows
-        // of chunk c + 1 in the ring.
+        // Per chunk of 128 columns a wave fetches a quarter of the token rows into the ring, two chunks ahead, and its weights into registers
+        // half a chunk at a time, as soon as the half before them in the same registers is used.
         auto load_t = [&](int c, int slot) {
 #pragma unroll
-            for (int b = 0; b < NB; ++b)
-                __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(tp[b] + (size_t)c * kFp8Block),
-                                                 (__attribute__((address_space(3))) void *)(ring + slot * kF8Slot + b * 4096 + wave * 1024), 16, 0, 0);
+            for (int b = 0; b < NB; ++b) {
+                const auto to = (__attribute__((address_space(3))) void *)(ring + slot * kF8Slot + b * 4096 + wave * 1024);
+                if constexpr (BIG) __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void *)(a.src + tp[b] + (size_t)c * kFp8Block), to, 16, 0, 0);
+                else __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, to, 16, tp[b], c * kFp8Block, 0, 0);
+            }
         };
         const uint32_t ring0 = lds_addr(ring), sw = (l32 >> 1) & 7;
         uint32_t ts[NB], wsc = 0;  // four chunks' scales
-        auto multiply = [&](const u32x4 (&w)[2][4], int c, int slot) {
+        auto multiply = [&](int c, int slot, bool more) {
             if ((c & 3) == 0) {
                 wsc = lds_read_b32(my_ws + c);
 #pragma unroll
@@ -181,26 +190,26 @@ struct F8Kernel {
                     acc[u][b] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wu, tb, acc[u][b], 0, 0, 0, sa, 0, (int)(ts[b] >> (8 * (c & 3))));
                 }
                 asm volatile("" : "+v"(acc[0][b]), "+v"(acc[1][b]));  // (here and not after later reads, whose fragments would all stay in registers)
+                if (b == NB - 1 && more) load_w(c + 1, m);
             };
             for_steps(step, std::make_integer_sequence<int, 2 * NB>{});
         };
         int slot = 0;
         // LEFT: chunks that follow this one, two at most; nothing is asked for past the last one
-        auto chunk = [&](const u32x4 (&w)[2][4], u32x4 (&next)[2][4], int c, auto left) {
+        auto chunk = [&](int c, auto left) {
             constexpr int LEFT = decltype(left)::value;
-            // chunk c's token rows (behind them: chunk c's weights and chunk c + 1's rows; of the first chunk see below)
+            // chunk c's token rows (asked for behind them: chunk c's weights and chunk c + 1's rows; of the first chunk see below)
             asm volatile("s_waitcnt vmcnt(%0)" ::"n"((LEFT >= 1 ? NB : 0) + 8) : "memory");
             asm volatile("s_barrier" ::: "memory");  // everyone's; and everyone is done with chunk c - 1
-            if constexpr (LEFT >= 2) load_t(min(c + 2, nk - 1), slot == 0 ? 2 : slot - 1);
-            if constexpr (LEFT >= 1) load_w(next, min(c + 1, nk - 1));
-            if (!ODD || c < nk) multiply(w, c, slot);  // (a single chunk: the two behind it are left out)
+            if constexpr (LEFT >= 2) load_t(c + 2, slot == 0 ? 2 : slot - 1);
+            multiply(c, slot, LEFT >= 1);
             slot = slot == 2 ? 0 : slot + 1;
         };
         constexpr std::integral_constant<int, 0> none{};
         constexpr std::integral_constant<int, 1> one{};
         constexpr std::integral_constant<int, 2> two{};
         load_t(0, 0);
-        load_t(min(1, nk - 1), 1);
+        if constexpr (!ONE) load_t(1, 1);
         // scales: one LDS row per token row, then one (two: gate, up) for the weights
         for (int i = tid; i < NB * 32 * (pitch / 4); i += kF8Threads) {
             const int r = i / (pitch / 4), c = i - r * (pitch / 4), rr = row0 + min(r, rows - 1);
@@ -219,21 +228,11 @@ struct F8Kernel {
         // The first chunk's weights were asked for before its token rows, so the count that a chunk waits for does not cover these: all but the
         // second chunk's rows are awaited here (a wave that fetches no scales has nothing else that waits).  And the scale tables are
         // written.  Both are met by the first barrier.
-        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(NB) : "memory");
+        asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(ONE ? 0 : NB) : "memory");
         int c = 0;
-        for (; c + 2 + ODD < nk; c += 2) {
-            chunk(wa[0], wa[1], c, two);
-            chunk(wa[1], wa[0], c + 1, two);
-        }
-        // (straight on: paths that meet again would hold all accumulators twice)
-        if constexpr (ODD) {
-            chunk(wa[0], wa[1], c, two);
-            chunk(wa[1], wa[0], c + 1, one);
-            chunk(wa[0], wa[1], c + 2, none);
-        } else {
-            chunk(wa[0], wa[1], c, one);
-            chunk(wa[1], wa[0], c + 1, none);
-        }
+        for (; c + 2 < nk; ++c) chunk(c, two);
+        if constexpr (!ONE) chunk(c++, one);
+        chunk(c, none);
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __syncthreads();  // everyone is done with the ring
         // acc[u][b][i]: unit row 8 (i / 4) + 4 half + i % 4, token row 32 b + l32
@@ -316,24 +315,25 @@ struct F8Kernel {
     }
 };
 
-template <int KIND, int ODD>
+template <int KIND, bool ONE, bool BIG>
 __global__ __launch_bounds__(kF8Threads, 2) void ffn_fp8_kernel(F8Args a)
 {
     extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
     F8Tiles t;
-    t.count(a.offsets, a.N);
+    t.count(a.offsets, a.N, a.tok);
     // the chip hands workgroups to its eight XCDs in turn: each takes a contiguous eighth of the items, so that the feature tiles of a
     // token tile and the token tiles of an expert meet in one L2
     const int items = t.total * a.nft, per = (items + 7) / 8, idx = blockIdx.x >> 3, item = (blockIdx.x & 7) * per + idx;
     if (idx >= per || item >= items) return;
     const int tile = item / a.nft, ft = item - tile * a.nft;
     const int3 at = t.locate(tile);
-    const F8Kernel<KIND, ODD> k = {a, lds, lds + kF8Ring, at.x, at.y, at.z, ft};
+    const F8Kernel<KIND, ONE, BIG> k = {a, lds, lds + kF8Ring, at.x, at.y, at.z, ft};
     const int nb = (at.z + 31) >> 5;
     if (nb == 1) k.template run<1>();
     else if (nb == 2) k.template run<2>();
     else if (nb == 3) k.template run<3>();
-    else k.template run<4>();
+    else if (nb == 4) k.template run<4>();
+    else k.template run<5>();
 }
 
 // scratch: token rows and scales, activations and scales, exponents of the expert outputs
@@ -358,7 +358,7 @@ static F8Ws fp8_ws(const zeda_layer_desc *d)
 }
 size_t fp8_ffn_ws_bytes(const zeda_layer_desc *d) { return fp8_ws(d).total; }
 
-template <int KIND, int ODD>
+template <int KIND, bool ONE, bool BIG = false>
 static int launch_f8_chunks(const F8Args &a, int S, hipStream_t s)
 {
     const int pitch = fp8_pitch(KIND == kF8GateUp ? a.H : a.Ip), tab = (kF8Tok + 2) * pitch, bytes = kF8Ring + (tab > 4 * kF8Tok * 4 ? tab : 4 * kF8Tok * 4);
@@ -367,19 +367,21 @@ static int launch_f8_chunks(const F8Args &a, int S, hipStream_t s)
     if (dev < 0) return ZEDA_EHIP;
     if (!done[dev]) {
         constexpr int most = kF8Ring + (kF8Tok + 2) * (kFp8MaxWidth / kFp8Block);
-        if (hipFuncSetAttribute((const void *)ffn_fp8_kernel<KIND, ODD>, hipFuncAttributeMaxDynamicSharedMemorySize, most) != hipSuccess) return ZEDA_EHIP;
+        if (hipFuncSetAttribute((const void *)ffn_fp8_kernel<KIND, ONE, BIG>, hipFuncAttributeMaxDynamicSharedMemorySize, most) != hipSuccess) return ZEDA_EHIP;
         done[dev] = true;
     }
-    const int64_t items = ((int64_t)S / kF8Tok + (a.N < S ? a.N : S)) * a.nft, grid = (items + 7) / 8 * 8;
+    const int64_t items = ((int64_t)S / a.tok + (a.N < S ? a.N : S)) * a.nft, grid = (items + 7) / 8 * 8;
     if (grid > 0x7fffffff) return ZEDA_EUNSUPPORTED;
-    ffn_fp8_kernel<KIND, ODD><<<(unsigned)grid, kF8Threads, bytes, s>>>(a);
+    ffn_fp8_kernel<KIND, ONE, BIG><<<(unsigned)grid, kF8Threads, bytes, s>>>(a);
     return last_launch_status();
 }
 
 template <int KIND>
 static int launch_f8(const F8Args &a, int S, hipStream_t s)
 {
-    return (KIND == kF8GateUp ? a.H : a.Ip) / kFp8Block % 2 ? launch_f8_chunks<KIND, 1>(a, S, s) : launch_f8_chunks<KIND, 0>(a, S, s);
+    // (a single chunk's token rows never pass 4 GiB: T * K < 2^24)
+    if (KIND == kF8GateUp && (int64_t)a.T * a.H >= (int64_t)1 << 32) return launch_f8_chunks<kF8GateUp, false, true>(a, S, s);
+    return (KIND == kF8GateUp ? a.H : a.Ip) == kFp8Block ? launch_f8_chunks<KIND, true>(a, S, s) : launch_f8_chunks<KIND, false>(a, S, s);
 }
 
 int launch_ffn_fp8(const zeda_layer_desc *d, const void *x, const zeda_fp8_experts *e, const int32_t *offsets, const int32_t *sorted_slot,
@@ -402,6 +404,11 @@ int launch_ffn_fp8(const zeda_layer_desc *d, const void *x, const zeda_fp8_exper
     a.w = (const uint8_t *)e->w_gateup; a.ws = (const uint8_t *)e->s_gateup;
     a.act = w + L.act; a.act_s = w + L.act_s;
     a.nft = Ip / kFp8Block;
+    // Tiles of up to 160 rows use each weight more often, tiles of up to 128 make more workgroups; by the work items that all slots would make.
+    // Whole layer, us, 128 / 160 rows: N=24, I=448, H=1152, 3000 tokens (280 items) 44.7 / 48.1; N=64, I=1536, H=2048, 2048 tokens (768) 149.3 /
+    // 150.9, 8192 skewed (3072) 225.1 / 226.9, 16384 (6144) 422.4 / 417.9; N=128, I=768, H=2048, 2048 tokens (768) 159.1 / 160.9, 4096 (1536) 202.3 /
+    // 202.3, 8192 (3072) 280.5 / 270.5, 16381 skewed (6144) 453.8 / 443.9
+    a.tok = (int64_t)S * a.nft < 128 * 3072 ? 128 : kF8Tok;
     if ((rc = launch_f8<kF8GateUp>(a, S, s)) != ZEDA_OK) return rc;
     a.src = a.act; a.src_s = a.act_s;
     a.w = (const uint8_t *)e->w_down; a.ws = (const uint8_t *)e->s_down;

@@ -312,6 +312,8 @@ def test_tiles_of_all_sizes_keep_their_bits_after_other_data(H, I):
     """Rows of one to four 32-row blocks per tile, and between the runs the same kernels on data whose every value is a NaN: what a workgroup
     finds in its shared memory must not reach the result."""
     loads = [1, 20, 40, 64, 70, 96, 100, 128, 5, 33, 129, 160] * 4
+    if H == 512:  # enough work items for tiles of 160 rows
+        loads += [161, 320, 2000] + [30000] * 7
     N, T = len(loads), sum(loads)
     w, d = _layer(T, H, I, N, 1, 1)
     qs = [zeda.zeda_quantize_weights_fp8(m.contiguous()) for m in synth.draw_experts(w, "cuda")]
@@ -331,6 +333,51 @@ def test_tiles_of_all_sizes_keep_their_bits_after_other_data(H, I):
     for rep in range(12):
         assert torch.isnan(run(bad)).all()
         assert torch.equal(run(x), first), rep
+
+
+def test_tiles_of_160_rows_give_what_tiles_of_128_give():
+    """Twice the experts' rows from one call with many work items (other tiles) against calls with few."""
+    loads = [159, 160, 161, 300, 128, 31, 0, 45]
+    H, I, N, many = 256, 128, len(loads), 60000
+    w, d = _layer(sum(loads), H, I, N + 1, 0, 1)
+    big = zeda.make_desc(sum(loads) + 8 * many, H, I, N + 1, 0, 1, "bf16")
+    assert big.T * 1 >= 128 * 3072
+    qs = [zeda.zeda_quantize_weights_fp8(m.contiguous()) for m in synth.draw_experts(w, "cuda")]
+    packed = zeda.zeda_pack_expert_weights_fp8(d, *[t for p in qs for t in p])
+    x = torch.randn(big.T, H, device="cuda").bfloat16()
+    outs = []
+    for desc, extra in ((d, 0), (big, 8 * many)):
+        ids = torch.tensor(np.repeat(np.arange(N + 1), loads + [extra]), dtype=torch.int32, device="cuda").view(desc.T, 1)
+        off, ss, _, nr = _dispatch(desc, ids)
+        y = torch.empty(desc.T, H, dtype=torch.bfloat16, device="cuda")
+        zeda.zeda_expert_ffn_fp8(desc, x, packed, off, ss, nr, y, torch.empty(zeda.expert_ffn_workspace_bytes_fp8(desc), dtype=torch.uint8, device="cuda"))
+        outs.append(y[: sum(loads)])
+    torch.cuda.synchronize()
+    assert torch.equal(*outs)
+
+
+def test_token_rows_past_4_gib():
+    """T * H >= 2^32: offsets of the quantised rows pass 32 bits; the last tokens against a call of their own."""
+    H, I, N, T = 16384, 64, 3, (1 << 18) + 700
+    x = torch.zeros(T, H, dtype=torch.bfloat16, device="cuda")
+    last = 1500
+    x[-last:] = torch.randn(last, H, device="cuda").bfloat16()
+    w, d = _layer(last, H, I, N, 0, 1)
+    qs = [zeda.zeda_quantize_weights_fp8(m.contiguous()) for m in synth.draw_experts(w, "cuda")]
+    packed = zeda.zeda_pack_expert_weights_fp8(d, *[t for p in qs for t in p])
+    ids = torch.tensor(np.arange(last) % N, dtype=torch.int32, device="cuda").view(last, 1)
+
+    def run(T, x, ids):
+        desc = zeda.make_desc(T, H, I, N, 0, 1, "bf16")
+        off, ss, sr, nr = _dispatch(desc, ids)
+        y = torch.empty(T, H, dtype=torch.bfloat16, device="cuda")
+        zeda.zeda_expert_ffn_fp8(desc, x, packed, off, ss, nr, y, torch.empty(zeda.expert_ffn_workspace_bytes_fp8(desc), dtype=torch.uint8, device="cuda"))
+        return y[sr.long()[-last:]]
+
+    want = run(last, x[-last:].contiguous(), ids)
+    got = run(T, x, torch.cat([torch.zeros(T - last, 1, dtype=torch.int32, device="cuda"), ids]))
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
 
 
 def test_a_slot_out_of_range_is_some_token():
