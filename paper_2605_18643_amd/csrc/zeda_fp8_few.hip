@@ -289,16 +289,16 @@ static int64_t few_tiles(const zeda_layer_desc *d)
 // activations: by the slots per expert if they fell evenly on all N + Z experts.  Every workgroup rounds the rows of its tile for
 // itself, which costs the more the wider the rows are, and tiles of 16 rows fetch an expert's weights once each; the tile kernels want
 // work items to fill the chip with.  Whole layer, us, tiles / here (half of the slots on zero experts):
-//   N=128, I=768, H=2048: 1 token 32.6 / 21.3, 16 63.5 / 60.3, 64 (3.2 slots) 122.5 / 114.2, 80 (4.0) 126.9 / 124.3, 100 (5.0) 130.4 / 132.8
-//   N=64, I=1536, H=2048: 1 token 34.5 / 23.4, 32 (1.3) 102.2 / 88.5, 64 (2.7) 120.8 / 117.5, 96 (4.0) 126.0 / 129.0
-//   N=32, I=1024, H=4096: 1 token 41.2 / 25.9, 4 (0.7) 52.5 / 51.4, 8 (1.3) 68.8 / 70.5
-//   N=24, I=448, H=1152, 96 items: 1 token 24.6 / 16.3, 64 (6.0) 29.9 / 26.5, 100 (9.4) 30.0 / 28.8, 160 (15) 30.2 / 32.5
-//   N=16, I=256, H=512, 32 items: 1 token 19.9 / 14.5, 400 (33) 22.6 / 19.8, 600 (50) 24.9 / 24.4, 900 (75) 26.9 / 26.8
+//   N=128, I=768, H=2048: 1 token 29.8 / 21.4, 16 64.3 / 60.0, 64 (3.2 slots) 118.1 / 114.8, 80 (4.0) 124.7 / 124.6, 100 (5.0) 129.6 / 132.6
+//   N=64, I=1536, H=2048: 1 token 30.6 / 23.4, 32 (1.3) 100.0 / 88.5, 64 (2.7) 116.5 / 117.2, 96 (4.0) 124.5 / 128.5
+//   N=32, I=1024, H=4096: 1 token 35.6 / 25.8, 4 (0.7) 48.6 / 51.1, 8 (1.3) 63.5 / 71.1
+//   N=24, I=448, H=1152, 96 items: 1 token 22.8 / 16.2, 64 (6.0) 28.3 / 26.4, 100 (9.4) 28.5 / 28.6, 160 (15) 28.6 / 32.4
+//   N=16, I=256, H=512, 32 items: 1 token 19.4 / 14.5, 400 (33) 22.1 / 19.8, 600 (50) 23.9 / 24.3, 900 (75) 25.9 / 27.0
 int64_t fp8_few_slots(const zeda_layer_desc *d)
 {
     if (few_rows_bytes(d->H) > 72 * 1024 || few_rows_bytes(fp8_cols(d->I)) > 72 * 1024) return 0;  // (two workgroups to a CU)
     const int64_t items = (int64_t)d->N * (fp8_cols(d->I) / kFp8Block);
-    const int64_t tenths = items <= 40 ? 600 : items <= 128 ? 110 : d->H > 2048 ? 10 : d->I > 1024 ? 32 : 42;
+    const int64_t tenths = items <= 40 ? 450 : items <= 128 ? 93 : d->H > 2048 ? 5 : d->I > 1024 ? 25 : 40;
     return tenths * ((int64_t)d->N + d->Z) / 10;
 }
 bool fp8_places(const zeda_layer_desc *d) { return fp8_few(d) && (int64_t)d->T * d->K <= kTileMaxSlots && few_tiles(d) * (fp8_cols(d->I) / 16) <= 7168; }
