@@ -61,6 +61,7 @@ struct RouteTables {
     size_t bytes() const { return (size_t)slices * Tpad * E * sizeof(float); }
 };
 RouteTables route_tables(const zeda_layer_desc *d);
+size_t route_tables_most(const zeda_layer_desc *d);  // bytes that the tables of no batch of up to T tokens pass
 int launch_route_tables(const zeda_layer_desc *d, const void *x, const void *wr, float *tables, hipStream_t s);
 // What a training step's selection leaves beside ids and gates: probs[T][NE]; per workgroup the sums of the probabilities of the tokens that
 // count (mask, may be NULL), part_p[NE], and part_c[NE + 1], their slots on every expert and their number; *done = 0.

@@ -860,6 +860,15 @@ RouteTables route_tables(const zeda_layer_desc *d)
     const RoutePlan p = route_plan(d, true);
     return {p.slices, route_tpad(d), E, 16 * p.tb};
 }
+// route_plan takes splits that fit into route_ws_bytes: at most eight slices of blocks of 32 tokens, blocks times slices within 256, so that no
+// split passes min(256 * blocks, 8192) rows.  Unlike that scratch, which shrinks where a longer batch takes fewer slices, this never
+// falls as T grows: callers size workspaces once, for their longest batch, whose router may need no tables.
+size_t route_tables_most(const zeda_layer_desc *d)
+{
+    if (d->dtype != ZEDA_BF16) return route_tables(d).bytes();
+    const size_t rows = (size_t)ceil_div(d->T, 32) * 256;
+    return (rows < 8192 ? rows : 8192) * route_row_bytes(d);
+}
 bool route_train_fused(const zeda_layer_desc *d) { return d->dtype == ZEDA_BF16 && route_plan(d, true).slices == 1; }
 int launch_route_train_fused(const zeda_layer_desc *d, const void *x, const void *wr, const float *bias, int32_t *ids, float *gates, const TrainOut &to,
                              hipStream_t s)

@@ -153,11 +153,7 @@ static TrainWs train_ws(const zeda_layer_desc *d)
     TrainWs w;
     size_t o = 0;
     auto take = [&](size_t bytes) { const size_t at = o; o += align_up(bytes ? bytes : 1, 256); return at; };
-    // (callers size workspaces once, for their longest batch: never less for a longer one, whose router may need no tables.  A split has at
-    // most eight slices and 4096 tokens times slices, whatever the batch)
-    const RouteTables t = route_tables(d);
-    const size_t rows = (size_t)ceil_div(d->T, 32) * 256;
-    w.tables = take(d->dtype == ZEDA_BF16 ? (rows < 4096 ? rows : 4096) * t.E * 4 : t.bytes());
+    w.tables = take(route_tables_most(d));
     w.part_p = take(nblk * NE * 4);
     w.part_c = take(nblk * (NE + 1) * 4);
     w.done = take(4);
@@ -180,6 +176,7 @@ int launch_route_train(const zeda_layer_desc *d, const void *x, const void *wr, 
         return last_launch_status();
     }
     const bool fused = route_train_fused(d);
+    if (!fused && t.bytes() > L.part_p - L.tables) return ZEDA_EWORKSPACE;  // (no plan is past route_tables_most)
     const int rows = fused ? ceil_div(d->T, t.tokens) : nblk;  // workgroups that select
     const int rc = fused ? launch_route_train_fused(d, x, wr, bias, ids, gates, to, s) : launch_route_tables(d, x, wr, tables, s);
     if (rc != ZEDA_OK) return rc;
