@@ -274,11 +274,11 @@ int zeda_moe_block_forward(const zeda_layer_desc *desc, const void *xn, void *x_
 
 /* Rows to 8 bits: q[rows, cols] e4m3 and scales[rows, ceil(cols/128)] bytes from x[rows, cols] of `dtype` (zeda_dtype).  A last
  * block may be shorter than 128.  cols % 8 == 0 (ZEDA_EUNSUPPORTED otherwise).  Infinities and no-numbers become no-numbers (0x7f,
- * 0xff) and do not count for the scale.  rows = 0 is a no-op. */
+ * 0xff) and do not count for the scale.  rows = 0 is a no-op (pointers may be NULL). */
 int zeda_quantize_rows_fp8(int32_t rows, int32_t cols, int32_t dtype, const void *x, void *q, uint8_t *scales, void *stream);
 
 /* Weights to 8 bits: `count` matrices w[count, rows, cols] of `dtype` to q[count, rows, cols] e4m3 under one scale per block of
- * 128 x 128, scales[count, ceil(rows/128), ceil(cols/128)].  cols % 8 == 0.  Otherwise as zeda_quantize_rows_fp8. */
+ * 128 x 128, scales[count, ceil(rows/128), ceil(cols/128)].  cols % 8 == 0.  count = 0 is a no-op.  Otherwise as zeda_quantize_rows_fp8. */
 int zeda_quantize_weights_fp8(int32_t count, int32_t rows, int32_t cols, int32_t dtype, const void *w, void *q, uint8_t *scales,
                               void *stream);
 

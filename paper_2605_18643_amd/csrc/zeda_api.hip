@@ -537,7 +537,8 @@ int zeda_pack_expert_weights(const zeda_layer_desc *desc, const void *w_gate, co
 
 int zeda_quantize_rows_fp8(int32_t rows, int32_t cols, int32_t dtype, const void *x, void *q, uint8_t *scales, void *stream)
 {
-    if (rows < 0 || cols < 1 || (dtype != ZEDA_F32 && dtype != ZEDA_BF16) || !x || !q || !scales || !aligned16(x) || !aligned16(q)) return ZEDA_EINVAL;
+    if (rows < 0 || cols < 1 || (dtype != ZEDA_F32 && dtype != ZEDA_BF16) || !aligned16(x) || !aligned16(q)) return ZEDA_EINVAL;
+    if (rows > 0 && (!x || !q || !scales)) return ZEDA_EINVAL;
     if (cols % 8 != 0) return ZEDA_EUNSUPPORTED;
     if (rows == 0) return ZEDA_OK;
     return launch_quantize_rows(rows, cols, dtype, x, q, cols, scales, ceil_div(cols, kFp8Block), (hipStream_t)stream);
@@ -545,8 +546,8 @@ int zeda_quantize_rows_fp8(int32_t rows, int32_t cols, int32_t dtype, const void
 
 int zeda_quantize_weights_fp8(int32_t count, int32_t rows, int32_t cols, int32_t dtype, const void *w, void *q, uint8_t *scales, void *stream)
 {
-    if (count < 0 || rows < 1 || cols < 1 || (dtype != ZEDA_F32 && dtype != ZEDA_BF16) || !w || !q || !scales || !aligned16(w) || !aligned16(q))
-        return ZEDA_EINVAL;
+    if (count < 0 || rows < 1 || cols < 1 || (dtype != ZEDA_F32 && dtype != ZEDA_BF16) || !aligned16(w) || !aligned16(q)) return ZEDA_EINVAL;
+    if (count > 0 && (!w || !q || !scales)) return ZEDA_EINVAL;
     if (cols % 8 != 0) return ZEDA_EUNSUPPORTED;
     if (count == 0) return ZEDA_OK;
     return launch_quantize_weights(count, rows, cols, dtype, w, q, scales, (hipStream_t)stream);
