@@ -472,7 +472,7 @@ def zeda_route_backward(desc, x, w_router, probs, topk_ids, topk_gates, token_ma
 def zeda_combine_backward(desc, d_out, y_slot, topk_ids, topk_gates, slot_to_row, x, d_gates, d_y_slot, dx, stream=None) -> None:
     """Backward of zeda_combine.  d_y_slot may be None; x and dx belong to EXPERT_COPY (None otherwise, dx None if not wanted)."""
     S, f, dt = desc.T * desc.K, torch.float32, _dtype_of(desc)
-    _typed("zeda_combine_backward", (d_out, dt, desc.T * desc.H), (topk_ids, torch.int32, S), (topk_gates, f, S), (slot_to_row, torch.int32, S),
+    _typed("zeda_combine_backward", (d_out, dt, desc.T * desc.H), (y_slot, dt, S * desc.H), (topk_ids, torch.int32, S), (topk_gates, f, S), (slot_to_row, torch.int32, S),
            (x, dt, desc.T * desc.H), (d_gates, f, S), (d_y_slot, dt, S * desc.H), (dx, dt, desc.T * desc.H))
     _check(lib().zeda_combine_backward(ctypes.byref(desc), _ptr(d_out), _ptr(y_slot), _ptr(topk_ids), _ptr(topk_gates), _ptr(slot_to_row), _ptr(x),
                                        _ptr(d_gates), _ptr(d_y_slot), _ptr(dx), _stream(stream)), "zeda_combine_backward")
