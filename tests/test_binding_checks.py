@@ -1,4 +1,6 @@
 """What the C side cannot see of a tensor, refused by the binding before anything is launched (no GPU)."""
+import ctypes
+
 import pytest
 import torch
 
@@ -27,3 +29,32 @@ def test_combine_backward_looks_at_the_expert_outputs(dtype):
     y = torch.zeros(12, 128, dtype=dt)
     for bad in (*_wrong(y), y.to(other), y[:6]):
         assert _refused(lambda: zeda.zeda_combine_backward(d, t["d_out"], bad, t["ids"], t["gates"], t["s2r"], None, t["d_gates"], t["dy"], None))
+
+
+def _layer(T=6, H=256, I=128, N=3, Z=2, K=2):
+    d = zeda.make_desc(T, H, I, N, Z, K, "bf16")
+    sizes = (ctypes.c_size_t * 4)()
+    assert zeda.lib().zeda_fp8_expert_bytes(ctypes.byref(d), sizes) == zeda.ZEDA_OK
+    experts = zeda.Fp8Experts([torch.zeros(n, dtype=torch.uint8) for n in sizes])
+    t = dict(x=torch.zeros(T, H, dtype=BF), wr=torch.zeros(N + Z, H, dtype=BF), bias=torch.zeros(N + Z), out=torch.zeros(T, H, dtype=BF), nr=torch.zeros(1, dtype=I32),
+             x_res=torch.zeros(T, H, dtype=BF), gamma=torch.zeros(H, dtype=BF), xn=torch.zeros(T, H, dtype=BF), off=torch.zeros(N + 1, dtype=I32),
+             ss=torch.zeros(T * K, dtype=I32), y=torch.zeros(T * K, H, dtype=BF), ws=torch.zeros(zeda.workspace_bytes_fp8(d), dtype=torch.uint8))
+
+    def calls(d=d, experts=experts, **kw):
+        a = {**t, **kw}
+        return {"ffn": lambda: zeda.zeda_expert_ffn_fp8(d, a["x"], experts, a["off"], a["ss"], a["nr"], a["y"], a["ws"]),
+                "forward": lambda: zeda.zeda_moe_forward_fp8(d, a["x"], a["wr"], a["bias"], experts, a["out"], a["nr"], a["ws"]),
+                "block": lambda: zeda.zeda_moe_block_forward_fp8(d, a["x"], a["x_res"], a["wr"], a["bias"], experts, a["gamma"], 1e-6, a["xn"], a["nr"], a["ws"])}
+
+    return d, t, calls
+
+
+TAKES = {"ffn": ("x", "off", "ss", "nr", "y"), "forward": ("x", "wr", "bias", "out", "nr"), "block": ("x", "x_res", "wr", "bias", "gamma", "xn", "nr")}
+
+
+@pytest.mark.parametrize("call", TAKES)
+def test_8_bit_layer_calls_look_at_their_tensors(call):
+    _, t, calls = _layer()
+    for n in TAKES[call]:
+        for bad in _wrong(t[n])[: 2 if t[n].numel() == 1 else 3]:
+            assert _refused(calls(**{n: bad})[call]), n
