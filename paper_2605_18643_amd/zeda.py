@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional
+from typing import Optional, Tuple
 
 import torch
 
@@ -47,13 +47,26 @@ class WsLayout(ctypes.Structure):
 
 
 class Fp8Experts(ctypes.Structure):
-    """Packed 8-bit expert weights (zeda_fp8_experts): the C struct, and the device buffers that it points to in `buffers`."""
+    """Packed 8-bit expert weights (zeda_fp8_experts): the C struct, and the device buffers that it points to in `buffers`.
+    desc: the layer that they were packed for (only its N, H and I count), which calls with another one are then refused by; without
+    it they are taken for any layer whose packed sizes they have."""
 
     _fields_ = [(n, ctypes.c_void_p) for n in ("w_gateup", "w_down", "s_gateup", "s_down")]
 
-    def __init__(self, buffers):
+    def __init__(self, buffers, desc: Optional[LayerDesc] = None):
         super().__init__(*[b.data_ptr() for b in buffers])
         self.buffers = tuple(buffers)
+        self.shape = None
+        if desc is not None:
+            self.check(desc, "Fp8Experts")
+            self.shape = (desc.N, desc.H, desc.I)
+
+    def check(self, desc: LayerDesc, where: str) -> None:
+        if self.shape is not None:
+            _need(self.shape == (desc.N, desc.H, desc.I), where)
+            return
+        sizes = fp8_expert_bytes(desc)
+        _need(len(self.buffers) == 4 and all(b.numel() * b.element_size() >= n and b.is_contiguous() for b, n in zip(self.buffers, sizes)), where)
 
 
 class ZedaError(RuntimeError):
@@ -385,6 +398,13 @@ def zeda_quantize_weights_fp8(w, stream=None):
     return q, scales
 
 
+def fp8_expert_bytes(desc: LayerDesc) -> Tuple[int, ...]:
+    """Sizes of the four buffers of packed 8-bit expert weights, in the order of Fp8Experts' fields."""
+    sizes = (ctypes.c_size_t * 4)()
+    _check(lib().zeda_fp8_expert_bytes(ctypes.byref(desc), sizes), "zeda_fp8_expert_bytes")
+    return tuple(sizes)
+
+
 def zeda_pack_expert_weights_fp8(desc, q_gate, s_gate, q_up, s_up, q_down, s_down, stream=None) -> Fp8Experts:
     """The experts' 8-bit weights in the layout of the kernels (allocates the buffers); row-major inputs as
     zeda_quantize_weights_fp8 gives them: q_gate, q_up [N, I, H], q_down [N, H, I]."""
@@ -392,9 +412,7 @@ def zeda_pack_expert_weights_fp8(desc, q_gate, s_gate, q_up, s_up, q_down, s_dow
     for t, shape in ((q_gate, (N, I, H)), (s_gate, (N, Ib, H // 128)), (q_up, (N, I, H)), (s_up, (N, Ib, H // 128)), (q_down, (N, H, I)),
                      (s_down, (N, H // 128, Ib))):
         _need(tuple(t.shape) == shape and t.element_size() == 1 and t.is_contiguous(), "zeda_pack_expert_weights_fp8")
-    sizes = (ctypes.c_size_t * 4)()
-    _check(lib().zeda_fp8_expert_bytes(ctypes.byref(desc), sizes), "zeda_fp8_expert_bytes")
-    e = Fp8Experts([torch.empty(n, dtype=torch.uint8, device=q_gate.device) for n in sizes])
+    e = Fp8Experts([torch.empty(n, dtype=torch.uint8, device=q_gate.device) for n in fp8_expert_bytes(desc)], desc)
     _check(lib().zeda_pack_expert_weights_fp8(ctypes.byref(desc), _ptr(q_gate), _ptr(s_gate), _ptr(q_up), _ptr(s_up), _ptr(q_down), _ptr(s_down),
                                               ctypes.byref(e), _stream(stream)), "zeda_pack_expert_weights_fp8")
     return e
@@ -417,6 +435,7 @@ def workspace_layout_fp8(desc: LayerDesc) -> WsLayout:
 def zeda_expert_ffn_fp8(desc, x, experts: Fp8Experts, expert_offsets, sorted_slot, num_real, y_slot, ws, stream=None) -> None:
     S, bf, i32 = desc.T * desc.K, torch.bfloat16, torch.int32
     _typed("zeda_expert_ffn_fp8", (x, bf, desc.T * desc.H), (expert_offsets, i32, desc.N + 1), (sorted_slot, i32, S), (num_real, i32, 1), (y_slot, bf, S * desc.H))
+    experts.check(desc, "zeda_expert_ffn_fp8")
     _check(lib().zeda_expert_ffn_fp8(ctypes.byref(desc), _ptr(x), ctypes.byref(experts), _ptr(expert_offsets), _ptr(sorted_slot), _ptr(num_real),
                                      _ptr(y_slot), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)), "zeda_expert_ffn_fp8")
 
@@ -424,6 +443,7 @@ def zeda_expert_ffn_fp8(desc, x, experts: Fp8Experts, expert_offsets, sorted_slo
 def zeda_moe_forward_fp8(desc, x, w_router, router_bias, experts: Fp8Experts, out, num_real_out, ws, stream=None) -> None:
     n, NE, bf = desc.T * desc.H, desc.N + desc.Z, torch.bfloat16
     _typed("zeda_moe_forward_fp8", (x, bf, n), (w_router, bf, NE * desc.H), (router_bias, torch.float32, NE), (out, bf, n), (num_real_out, torch.int32, 1))
+    experts.check(desc, "zeda_moe_forward_fp8")
     _check(lib().zeda_moe_forward_fp8(ctypes.byref(desc), _ptr(x), _ptr(w_router), _ptr(router_bias), ctypes.byref(experts), _ptr(out),
                                       _ptr(num_real_out), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)), "zeda_moe_forward_fp8")
 
@@ -434,6 +454,7 @@ def zeda_moe_block_forward_fp8(desc, xn, x_res, w_router, router_bias, experts: 
     n, NE, bf = desc.T * desc.H, desc.N + desc.Z, torch.bfloat16
     _typed("zeda_moe_block_forward_fp8", (xn, bf, n), (x_res, bf, n), (w_router, bf, NE * desc.H), (router_bias, torch.float32, NE), (gamma_next, bf, desc.H),
            (xn_next, bf, n), (num_real_out, torch.int32, 1))
+    experts.check(desc, "zeda_moe_block_forward_fp8")
     _check(lib().zeda_moe_block_forward_fp8(ctypes.byref(desc), _ptr(xn), _ptr(x_res), _ptr(w_router), _ptr(router_bias), ctypes.byref(experts),
                                             _ptr(gamma_next), float(eps), _ptr(xn_next), _ptr(num_real_out), _ptr(ws),
                                             ws.numel() * ws.element_size(), _stream(stream)), "zeda_moe_block_forward_fp8")

@@ -31,11 +31,15 @@ def test_combine_backward_looks_at_the_expert_outputs(dtype):
         assert _refused(lambda: zeda.zeda_combine_backward(d, t["d_out"], bad, t["ids"], t["gates"], t["s2r"], None, t["d_gates"], t["dy"], None))
 
 
-def _layer(T=6, H=256, I=128, N=3, Z=2, K=2):
-    d = zeda.make_desc(T, H, I, N, Z, K, "bf16")
+def _experts(d, short=None, **kw):
     sizes = (ctypes.c_size_t * 4)()
     assert zeda.lib().zeda_fp8_expert_bytes(ctypes.byref(d), sizes) == zeda.ZEDA_OK
-    experts = zeda.Fp8Experts([torch.zeros(n, dtype=torch.uint8) for n in sizes])
+    return zeda.Fp8Experts([torch.zeros(n - (i == short), dtype=torch.uint8) for i, n in enumerate(sizes)], **kw)
+
+
+def _layer(T=6, H=256, I=128, N=3, Z=2, K=2):
+    d = zeda.make_desc(T, H, I, N, Z, K, "bf16")
+    experts = _experts(d)
     t = dict(x=torch.zeros(T, H, dtype=BF), wr=torch.zeros(N + Z, H, dtype=BF), bias=torch.zeros(N + Z), out=torch.zeros(T, H, dtype=BF), nr=torch.zeros(1, dtype=I32),
              x_res=torch.zeros(T, H, dtype=BF), gamma=torch.zeros(H, dtype=BF), xn=torch.zeros(T, H, dtype=BF), off=torch.zeros(N + 1, dtype=I32),
              ss=torch.zeros(T * K, dtype=I32), y=torch.zeros(T * K, H, dtype=BF), ws=torch.zeros(zeda.workspace_bytes_fp8(d), dtype=torch.uint8))
@@ -58,3 +62,25 @@ def test_8_bit_layer_calls_look_at_their_tensors(call):
     for n in TAKES[call]:
         for bad in _wrong(t[n])[: 2 if t[n].numel() == 1 else 3]:
             assert _refused(calls(**{n: bad})[call]), n
+
+
+@pytest.mark.parametrize("call", TAKES)
+def test_experts_packed_for_another_layer_are_refused(call):
+    d, t, calls = _layer()
+    # buffers that a caller has kept: by their sizes
+    for short in range(4):
+        assert _refused(calls(experts=_experts(d, short=short))[call])
+    assert _refused(calls(experts=_experts(zeda.make_desc(0, 128, 128, 3, 0, 1, "bf16")))[call])
+    assert _refused(calls(experts=zeda.Fp8Experts([]))[call])
+    # packed by the binding: by the layer's shape, where sizes are alike too
+    for N, H, I in ((4, 256, 128), (3, 256, 192), (3, 384, 128), (3, 128, 256), (1, 256, 384)):
+        other = zeda.make_desc(0, H, I, N, 0, 1, "bf16")
+        assert _refused(calls(experts=_experts(other, desc=other))[call]), (N, H, I)
+
+
+def test_buffers_too_small_for_the_descriptor_make_no_experts():
+    d = zeda.make_desc(0, 256, 128, 3, 0, 1, "bf16")
+    for short in range(4):
+        assert _refused(lambda: _experts(d, short=short, desc=d))
+    e = _experts(d, desc=d)
+    assert e.shape == (3, 256, 128) and e.w_gateup == e.buffers[0].data_ptr()
