@@ -433,16 +433,16 @@ def workspace_layout_fp8(desc: LayerDesc) -> WsLayout:
 
 
 def zeda_expert_ffn_fp8(desc, x, experts: Fp8Experts, expert_offsets, sorted_slot, num_real, y_slot, ws, stream=None) -> None:
-    S, bf, i32 = desc.T * desc.K, torch.bfloat16, torch.int32
-    _typed("zeda_expert_ffn_fp8", (x, bf, desc.T * desc.H), (expert_offsets, i32, desc.N + 1), (sorted_slot, i32, S), (num_real, i32, 1), (y_slot, bf, S * desc.H))
+    S, dt, i32 = desc.T * desc.K, _dtype_of(desc), torch.int32
+    _typed("zeda_expert_ffn_fp8", (x, dt, desc.T * desc.H), (expert_offsets, i32, desc.N + 1), (sorted_slot, i32, S), (num_real, i32, 1), (y_slot, dt, S * desc.H))
     experts.check(desc, "zeda_expert_ffn_fp8")
     _check(lib().zeda_expert_ffn_fp8(ctypes.byref(desc), _ptr(x), ctypes.byref(experts), _ptr(expert_offsets), _ptr(sorted_slot), _ptr(num_real),
                                      _ptr(y_slot), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)), "zeda_expert_ffn_fp8")
 
 
 def zeda_moe_forward_fp8(desc, x, w_router, router_bias, experts: Fp8Experts, out, num_real_out, ws, stream=None) -> None:
-    n, NE, bf = desc.T * desc.H, desc.N + desc.Z, torch.bfloat16
-    _typed("zeda_moe_forward_fp8", (x, bf, n), (w_router, bf, NE * desc.H), (router_bias, torch.float32, NE), (out, bf, n), (num_real_out, torch.int32, 1))
+    n, NE, dt = desc.T * desc.H, desc.N + desc.Z, _dtype_of(desc)
+    _typed("zeda_moe_forward_fp8", (x, dt, n), (w_router, dt, NE * desc.H), (router_bias, torch.float32, NE), (out, dt, n), (num_real_out, torch.int32, 1))
     experts.check(desc, "zeda_moe_forward_fp8")
     _check(lib().zeda_moe_forward_fp8(ctypes.byref(desc), _ptr(x), _ptr(w_router), _ptr(router_bias), ctypes.byref(experts), _ptr(out),
                                       _ptr(num_real_out), _ptr(ws), ws.numel() * ws.element_size(), _stream(stream)), "zeda_moe_forward_fp8")
@@ -451,9 +451,9 @@ def zeda_moe_forward_fp8(desc, x, w_router, router_bias, experts: Fp8Experts, ou
 def zeda_moe_block_forward_fp8(desc, xn, x_res, w_router, router_bias, experts: Fp8Experts, gamma_next, eps: float, xn_next, num_real_out, ws,
                                stream=None) -> None:
     """zeda_moe_block_forward with 8-bit experts."""
-    n, NE, bf = desc.T * desc.H, desc.N + desc.Z, torch.bfloat16
-    _typed("zeda_moe_block_forward_fp8", (xn, bf, n), (x_res, bf, n), (w_router, bf, NE * desc.H), (router_bias, torch.float32, NE), (gamma_next, bf, desc.H),
-           (xn_next, bf, n), (num_real_out, torch.int32, 1))
+    n, NE, dt = desc.T * desc.H, desc.N + desc.Z, _dtype_of(desc)
+    _typed("zeda_moe_block_forward_fp8", (xn, dt, n), (x_res, dt, n), (w_router, dt, NE * desc.H), (router_bias, torch.float32, NE), (gamma_next, dt, desc.H),
+           (xn_next, dt, n), (num_real_out, torch.int32, 1))
     experts.check(desc, "zeda_moe_block_forward_fp8")
     _check(lib().zeda_moe_block_forward_fp8(ctypes.byref(desc), _ptr(xn), _ptr(x_res), _ptr(w_router), _ptr(router_bias), ctypes.byref(experts),
                                             _ptr(gamma_next), float(eps), _ptr(xn_next), _ptr(num_real_out), _ptr(ws),

@@ -84,3 +84,15 @@ def test_buffers_too_small_for_the_descriptor_make_no_experts():
         assert _refused(lambda: _experts(d, short=short, desc=d))
     e = _experts(d, desc=d)
     assert e.shape == (3, 256, 128) and e.w_gateup == e.buffers[0].data_ptr()
+
+
+def test_fp32_layers_are_unsupported_not_ill_typed(monkeypatch):
+    """8-bit calls with an fp32 descriptor and fp32 tensors: what the header says of the descriptor."""
+    monkeypatch.setattr(zeda, "_stream", lambda stream: 0)  # (the library refuses before it looks at the stream)
+    d, t, calls = _layer()
+    f32 = zeda.make_desc(6, 256, 128, 3, 2, 2, "f32")
+    wide = {n: v.float() for n, v in t.items() if v.dtype == BF}
+    for call in calls(d=f32, experts=_experts(d, desc=d), **wide).values():
+        with pytest.raises(zeda.ZedaError) as e:
+            call()
+        assert e.value.status == zeda.ZEDA_EUNSUPPORTED
