@@ -6,6 +6,7 @@ raises, and nothing here computes on the CPU.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Optional, Tuple
@@ -189,6 +190,12 @@ def _stream(stream) -> int:
     return torch.cuda.current_stream().cuda_stream if raw is None else raw(torch.cuda.current_device())
 
 
+def _on(stream):
+    """Context for allocations that a call on `stream` fills: they come from that stream's blocks.  One of the current stream's may have been
+    freed with work on it still queued there, which the call on `stream` would not wait for."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
 def _check(rc: int, where: str) -> None:
     if rc != ZEDA_OK:
         raise ZedaError(rc, where)
@@ -333,11 +340,12 @@ def zeda_routing_stats(desc, x, w_router, router_bias, alpha=1.0, w=1.0, stream=
     """Section 2.2 statistics over the batch of all tokens; allocates the outputs and the scratch.
     Returns device tensors (f[N+Z], P[N+Z], summary[7] = f_E, P_E, f_Z, P_Z, r_ZE, L_A, L_GA)."""
     NE = desc.N + desc.Z
-    f = torch.empty(NE, dtype=torch.float32, device=x.device)
-    P = torch.empty(NE, dtype=torch.float32, device=x.device)
-    summary = torch.empty(7, dtype=torch.float32, device=x.device)
     nbytes = int(lib().zeda_routing_stats_workspace_bytes(ctypes.byref(desc)))
-    ws = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=x.device)
+    with _on(stream):
+        f = torch.empty(NE, dtype=torch.float32, device=x.device)
+        P = torch.empty(NE, dtype=torch.float32, device=x.device)
+        summary = torch.empty(7, dtype=torch.float32, device=x.device)
+        ws = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=x.device)
     _check(lib().zeda_routing_stats(ctypes.byref(desc), _ptr(x), _ptr(w_router), _ptr(router_bias), float(alpha), float(w),
                                     _ptr(f), _ptr(P), _ptr(summary), _ptr(ws), ws.numel(), _stream(stream)),
            "zeda_routing_stats")
@@ -346,7 +354,8 @@ def zeda_routing_stats(desc, x, w_router, router_bias, alpha=1.0, w=1.0, stream=
 
 def zeda_init_zero_expert_rows(desc, w_router, normals, stream=None):
     """Fills rows N.. of w_router in place (see include/zeda.h); returns the device tensor {mean, variance}."""
-    stats = torch.empty(2, dtype=torch.float32, device=w_router.device)
+    with _on(stream):
+        stats = torch.empty(2, dtype=torch.float32, device=w_router.device)
     _check(lib().zeda_init_zero_expert_rows(ctypes.byref(desc), _ptr(w_router), _ptr(normals), _ptr(stats), _stream(stream)),
            "zeda_init_zero_expert_rows")
     return stats
@@ -354,7 +363,8 @@ def zeda_init_zero_expert_rows(desc, w_router, normals, stream=None):
 
 def zeda_pack_expert_weights(desc, w_gate, w_up, w_down, stream=None):
     """Tiled copies of the three expert tensors (any of them may be None); allocates the outputs."""
-    outs = [None if w is None else torch.empty_like(w) for w in (w_gate, w_up, w_down)]
+    with _on(stream):
+        outs = [None if w is None else torch.empty_like(w) for w in (w_gate, w_up, w_down)]
     _check(lib().zeda_pack_expert_weights(ctypes.byref(desc), _ptr(w_gate), _ptr(w_up), _ptr(w_down), _ptr(outs[0]),
                                           _ptr(outs[1]), _ptr(outs[2]), _stream(stream)), "zeda_pack_expert_weights")
     return tuple(outs)
@@ -381,8 +391,9 @@ def zeda_quantize_rows_fp8(x, stream=None):
     x is nearly q * 2^(scale - 127)."""
     _need(_is_float_buffer(x, 2), "zeda_quantize_rows_fp8")
     rows, cols = x.shape
-    q = torch.empty((rows, cols), dtype=torch.float8_e4m3fn, device=x.device)
-    scales = torch.empty((rows, -(-cols // 128)), dtype=torch.uint8, device=x.device)
+    with _on(stream):
+        q = torch.empty((rows, cols), dtype=torch.float8_e4m3fn, device=x.device)
+        scales = torch.empty((rows, -(-cols // 128)), dtype=torch.uint8, device=x.device)
     _check(lib().zeda_quantize_rows_fp8(rows, cols, _dtype_code(x), _ptr(x), _ptr(q), _ptr(scales), _stream(stream)), "zeda_quantize_rows_fp8")
     return q, scales
 
@@ -391,8 +402,9 @@ def zeda_quantize_weights_fp8(w, stream=None):
     """w [count, rows, cols] (bf16 or fp32, contiguous) -> (q float8_e4m3fn like w, scales uint8 [count, ceil(rows / 128), ceil(cols / 128)])."""
     _need(_is_float_buffer(w, 3), "zeda_quantize_weights_fp8")
     count, rows, cols = w.shape
-    q = torch.empty((count, rows, cols), dtype=torch.float8_e4m3fn, device=w.device)
-    scales = torch.empty((count, -(-rows // 128), -(-cols // 128)), dtype=torch.uint8, device=w.device)
+    with _on(stream):
+        q = torch.empty((count, rows, cols), dtype=torch.float8_e4m3fn, device=w.device)
+        scales = torch.empty((count, -(-rows // 128), -(-cols // 128)), dtype=torch.uint8, device=w.device)
     _check(lib().zeda_quantize_weights_fp8(count, rows, cols, _dtype_code(w), _ptr(w), _ptr(q), _ptr(scales), _stream(stream)),
            "zeda_quantize_weights_fp8")
     return q, scales
@@ -412,7 +424,8 @@ def zeda_pack_expert_weights_fp8(desc, q_gate, s_gate, q_up, s_up, q_down, s_dow
     for t, shape in ((q_gate, (N, I, H)), (s_gate, (N, Ib, H // 128)), (q_up, (N, I, H)), (s_up, (N, Ib, H // 128)), (q_down, (N, H, I)),
                      (s_down, (N, H // 128, Ib))):
         _need(tuple(t.shape) == shape and t.element_size() == 1 and t.is_contiguous(), "zeda_pack_expert_weights_fp8")
-    e = Fp8Experts([torch.empty(n, dtype=torch.uint8, device=q_gate.device) for n in fp8_expert_bytes(desc)], desc)
+    with _on(stream):
+        e = Fp8Experts([torch.empty(n, dtype=torch.uint8, device=q_gate.device) for n in fp8_expert_bytes(desc)], desc)
     _check(lib().zeda_pack_expert_weights_fp8(ctypes.byref(desc), _ptr(q_gate), _ptr(s_gate), _ptr(q_up), _ptr(s_up), _ptr(q_down), _ptr(s_down),
                                               ctypes.byref(e), _stream(stream)), "zeda_pack_expert_weights_fp8")
     return e
