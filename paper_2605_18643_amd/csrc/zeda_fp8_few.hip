@@ -285,21 +285,30 @@ static int64_t few_tiles(const zeda_layer_desc *d)
     return (slots < d->N ? slots : d->N) + slots / kF8FewRows;
 }
 
-// Where these kernels beat the tile kernels, which quantise the tokens in a launch of their own and take a workgroup per 128
-// activations: by the slots per expert if they fell evenly on all N + Z experts.  Every workgroup rounds the rows of its tile for
-// itself, which costs the more the wider the rows are, and tiles of 16 rows fetch an expert's weights once each; the tile kernels want
-// work items to fill the chip with.  Whole layer, us, tiles / here (half of the slots on zero experts):
-//   N=128, I=768, H=2048: 1 token 29.8 / 21.4, 16 64.3 / 60.0, 64 (3.2 slots) 118.1 / 114.8, 80 (4.0) 124.7 / 124.6, 100 (5.0) 129.6 / 132.6
-//   N=64, I=1536, H=2048: 1 token 30.6 / 23.4, 32 (1.3) 100.0 / 88.5, 64 (2.7) 116.5 / 117.2, 96 (4.0) 124.5 / 128.5
-//   N=32, I=1024, H=4096: 1 token 35.6 / 25.8, 4 (0.7) 48.6 / 51.1, 8 (1.3) 63.5 / 71.1
-//   N=24, I=448, H=1152, 96 items: 1 token 22.8 / 16.2, 64 (6.0) 28.3 / 26.4, 100 (9.4) 28.5 / 28.6, 160 (15) 28.6 / 32.4
-//   N=16, I=256, H=512, 32 items: 1 token 19.4 / 14.5, 400 (33) 22.1 / 19.8, 600 (50) 23.9 / 24.3, 900 (75) 25.9 / 27.0
+// Up to how many slots these kernels beat the tile kernels, which quantise the tokens in a launch of their own and take a workgroup per 128
+// activations.  Every workgroup rounds the rows of its tile for itself, slots * Ip / 16 * H values in gate/up alone, and has a fixed cost like
+// that of some 256 columns more in both directions: at slots * (Ip + 256) * (H + 256) of about 2.8e8 that is what the launches saved and a chip
+// filled with more workgroups are worth, whatever the number of experts.  Where the layer's weights are past the last-level cache
+// (256 MiB) twice over, their streaming hides the rounding as long as tiles of 16 rows seldom fetch an expert's weights twice and a
+// workgroup's weights (32 H bytes) are more than its latency: up to 3.25 slots per expert if they fell evenly on all N + Z.
+// Whole layer, us, tiles / here, weights from HBM (half of the slots on zero experts), up to the slots in brackets here:
+//   N=16, I=1024, H=4096 (50): 16 slots 49.0 / 35.5, 48 55.2 / 55.2, 80 59.6 / 62.7;  I=256 (125): 120 46.6 / 38.4, 800 52.3 / 79.6
+//   N=24, I=448, H=4096 (83): 60 53.6 / 44.7, 288 57.9 / 62.4;  H=1152 (258): 192 32.4 / 27.0, 480 33.2 / 34.0
+//   N=64, I=512, H=1024 (284): 160 40.0 / 39.3, 320 41.9 / 45.0;  N=30, I=256, H=256 (1068): 400 22.9 / 20.5, 1200 23.8 / 23.9
+//   N=200, I=64, H=128 (1898): 2000 25.7 / 27.9, 8800 29.4 / 39.7;  N=1, I=2048, H=2048 (52): 35 41.4 / 34.4, 60 41.7 / 39.2
+//   N=128, I=768, H=2048 (520): 8 32.7 / 26.3, 128 67.4 / 58.6, 512 114.0 / 115.1, 640 119.5 / 126.1
+//   N=64, I=1536, H=2048 (312): 4 31.8 / 23.8, 128 85.1 / 79.6, 256 111.0 / 113.9, 384 123.1 / 127.2
+// Over 485 other shapes (N 4 to 220, I 128 to 2176, H 384 to 4480, 0.4 to 35 slots per expert) what is chosen is 0.6 % behind the better kernels on
+// average and 41 % at worst; 1.5 and 51 % where one layer's weights stay in the cache from call to call.
+// Above 45 slots per expert the tile kernels keep every call that they have had (one to three small experts would gain: N=3, I=512, H=512,
+// 400 slots 29.2 / 22.8).
 int64_t fp8_few_slots(const zeda_layer_desc *d)
 {
     if (few_rows_bytes(d->H) > 72 * 1024 || few_rows_bytes(fp8_cols(d->I)) > 72 * 1024) return 0;  // (two workgroups to a CU)
-    const int64_t items = (int64_t)d->N * (fp8_cols(d->I) / kFp8Block);
-    const int64_t tenths = items <= 40 ? 450 : items <= 128 ? 93 : d->H > 2048 ? 5 : d->I > 1024 ? 25 : 40;
-    return tenths * ((int64_t)d->N + d->Z) / 10;
+    const int64_t H = d->H, Ip = fp8_cols(d->I), NE = (int64_t)d->N + d->Z;
+    const int64_t rounded = 280000000 / ((H + 256) * (Ip + 256)), most = rounded < 45 * NE ? rounded : 45 * NE;
+    const int64_t hidden = d->N * 3 * H * Ip >= 500000000 && H > 1024 ? 13 * NE / 4 : 0;
+    return most > hidden ? most : hidden;
 }
 bool fp8_places(const zeda_layer_desc *d) { return fp8_few(d) && (int64_t)d->T * d->K <= kTileMaxSlots && few_tiles(d) * (fp8_cols(d->I) / 16) <= 7168; }
 bool fp8_selects(const zeda_layer_desc *d)

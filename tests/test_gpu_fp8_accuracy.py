@@ -29,7 +29,7 @@ def _error(T, H, I, N, Z, K, seed):
     return harness.rel_l2(out.double().cpu().numpy(), want)
 
 
-@pytest.mark.parametrize("T, seeds", [(1, 8), (16, 2)])
+@pytest.mark.parametrize("T, seeds", [(1, 8), (8, 3)])
 def test_short_batches_are_as_exact_as_fp32_sums(T, seeds):
     errors = [_error(T, 2048, 768, 24, 8, 8, seed) for seed in range(10, 10 + seeds)]
     print(T, errors, flush=True)
