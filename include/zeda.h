@@ -263,7 +263,8 @@ int zeda_moe_block_forward(const zeda_layer_desc *desc, const void *xn, void *x_
  * a scale, a power of two held as one byte s:  value = e4m3 * 2^(s - 127).  With Q(v) = rounding to the nearest such value
  * (ties to even) under the least power of two that keeps the block's largest finite magnitude within 448 (at least 2^-126):
  *        xq = Q(x) per token and 128 columns,   h = silu(G xq) .* (U xq),   E(x) = D Q(h),
- * where G, U, D are stored under one scale per 128 x 128 block.  Sums are fp32; in G xq and U xq of small batches as exact as fp32 is, else
+ * where G, U, D are stored under one scale per 128 x 128 block.  Sums are fp32; in G xq and U xq of small batches (where
+ * these end goes by T K, H, I and N + Z; none above H or I = 4480) as exact as fp32 is, else
  * with the products' bits that the 8-bit matrix instruction keeps, within about 13 binades of the largest product of a group:
  * relative to the root mean square of a sum that is 1.4e-5, which moves one activation in some thousands to the neighbouring e4m3
  * value (the result is then about 2.0e-3 off the formula, against 1.7e-3 for the rounding to bf16 alone).  h is rounded once, from fp32.  An infinity or
@@ -321,7 +322,8 @@ int zeda_moe_block_forward_fp8(const zeda_layer_desc *desc, const void *xn, void
 /* ---------------------------------------------------------------------------------------------------------------------
  * Training the router (Section 2.2): the balance losses with their gradient, and the gradient of the routing weights of Eq. 1.
  * One training step: zeda_route_train, zeda_dispatch, zeda_expert_ffn (or zeda_expert_ffn_fp8: experts frozen in 8 bits),
- * zeda_combine; then zeda_combine_backward and zeda_route_backward.
+ * zeda_combine; then zeda_combine_backward and zeda_route_backward.  No call carries the gradient of the expert outputs on to x: what reaches
+ * x is the router's share and, with copy experts, theirs.
  * ------------------------------------------------------------------------------------------------------------------- */
 
 /* zeda_route for a training step: topk_ids and topk_gates as there (the sums are those of zeda_route with scratch), and

@@ -9,7 +9,8 @@
 // other's products.
 // What bounds it: with up to 128 rows an expert the weights from HBM (997 tokens, N=64, I=1536, H=2048: gate/up 403 MB in 77 us = 5.2 TB/s, the
 // rate of a large copy).  4096 tokens of N=128, I=768 have 128 rows an expert on average, so every second expert of its tiles of 128 needs a
-// second one: gate/up 103 us, down 64; 16381 skewed tokens 167-271 and 123-199 us by the run's clock, the matrix pipes busy 53 and 33 % of the
+// second one: gate/up 103 us, down 64 (with tiles of 160, which hardly need one, the same, in 1.5 rounds of workgroups instead of 2.2).  16381 skewed
+// tokens with 51318 slots on normal experts: 164-207 and 123-146 us, with 72983 212-288 and 165-208, the matrix pipes busy 53 and 33 % of the
 // cycles (down writes 16 bits a product of 768 terms).
 // What the compiler must not see as flat: token rows fetched by global loads into LDS made it wait for everything in flight before the first
 // product of every chunk (4096 tokens, whole layer, 205 us against 202; 8192 tokens 283 against 270; 16381 470 against 444).
